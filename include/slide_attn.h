@@ -303,6 +303,101 @@ int slide_attn_fwd_nhwc(const void* q, const void* k, const void* v,
 int slide_attn_fwd_traffic_probe(const void* q, const void* k, const void* v, void* out,
                                  int B, int H, int W, int C, int heads, int mode, void* stream);
 
+/*
+ * Region attention: attention that reaches further than a window at the cost of a few regions.  Maps of queries and of keys are
+ * cut into regions of pixels; every region of queries carries a list of topk regions of keys, picked by a cheap score, and its
+ * rows attend the keys of those regions and no others.  A sequence is a map of height 1; one new token over what came before is a
+ * query map of one pixel.
+ *
+ * Layout: channels last.  q is [B, q_h, q_w, heads * head_dim], k and v are [B, k_h, k_w, kv_heads * head_dim]; heads is a
+ * multiple of kv_heads, and query heads [m * g, (m + 1) * g), g = heads / kv_heads, share key head m.  The channels of a pixel are
+ * contiguous; pixels are q_pixel elements apart in raster order and images q_image (likewise k, v), so q, k and v may be parts
+ * of one projection's output, or the filled part of a longer cache; image strides may be 0 (one map for the whole batch).
+ * out, dout and the gradients are contiguous.
+ * Regions: q_region_h x q_region_w pixels, in raster order, ragged at the right and bottom edge, G in all; a region larger than
+ * its map counts as the map.  Regions of keys likewise, J in all.
+ * index: int32 [B, kv_heads, G, topk]; an entry outside [0, J) is skipped, one that is listed twice counts twice.
+ * q_size, k_size: int32 [B, 2] on the device or NULL: the valid height and width of every image (clamped to the map), where a
+ * batch is padded at the right and bottom.  Pixels outside are never read as keys, whatever they hold; as queries they get
+ * zeros (lse: -infinity) and pass nothing to any gradient.  A row that has no key at all gets the same.
+ * scale: of the logits; 0 stands for 1/sqrt(head_dim).
+ * dropout: of the attention weights, in [0, 1); it is rounded to t / 65536, and weights that are kept are multiplied by
+ * 65536 / (65536 - t).  The mask is a function of seed, offset and the weight's place, and is never stored: the backward draws
+ * it again and has to be given the same values.  Row r = place in the query region * g + head in the group, key n = place in
+ * the key region (places count region_w to a row, region clamped as above): weight (b, m, region i, r, region j, n) is kept if
+ * half word 4 (r % 2) + n % 4 of the four words of Philox-4x32-7 with key seed and counter
+ *     (j * ceil(key places / 4) + n / 4,  i * ceil(rows / 2) + r / 2,  b * kv_heads + m,  offset)
+ * is at least t (half word 2 w + 1 is the upper half of word w).  offset: the number of the call, plus the low 32 bits of what
+ * offset_device (one integer on the device, or NULL) holds when the kernels run: a captured graph draws new masks with it.
+ *
+ * Limits: head_dim 1..128, topk 1..1024, fewer than 2^29 pixels per map; slide_region_select: at most 16384 regions of keys.
+ * SLIDE_ERR_SHAPE otherwise, and for a dropout outside [0, 1) or one that rounds to 1, a negative or NaN scale, and strides that
+ * let pixels of one map overlap.  Products are formed from the activations as they are (bf16: exactly), sums and softmax
+ * statistics are float32; for bf16 the attention weights and the logits' gradients are rounded to bf16 before the products with
+ * v, k, q and dout.  Results are reproducible run to run.
+ */
+typedef struct {
+    int B, heads, kv_heads, head_dim;
+    int q_h, q_w, k_h, k_w;
+    int q_region_h, q_region_w, k_region_h, k_region_w;
+    int topk;
+    int dtype;                                  /* of q, k, v, out, dout and the gradients */
+    long long q_pixel, q_image, k_pixel, k_image, v_pixel, v_image;
+    const int* q_size;
+    const int* k_size;
+    float scale;
+    float dropout;
+    unsigned long long seed;
+    unsigned int offset;
+    const long long* offset_device;
+} slide_region_problem;
+
+typedef enum { SLIDE_REGION_SELECT = 0, SLIDE_REGION_FWD = 1, SLIDE_REGION_BWD = 2 } slide_region_call;
+
+/* Bytes of device scratch, 16-byte aligned, that the call (a slide_region_call) needs; 0 for invalid arguments or if it needs
+ * none.  Launches nothing; reads the compute-unit count of the current device (256 if there is none). */
+size_t slide_region_workspace_bytes(const slide_region_problem* p, int call);
+
+/*
+ * The lists: for every group (image, key head m, region i of queries) the topk regions j of keys with the highest
+ *     (sum of q over the region's valid pixels and the group's g heads) . (sum of k over j's valid pixels) / (their number),
+ * ties to the lowest j, a NaN ranking as -infinity; regions without a valid pixel are never picked, and a region of queries
+ * without one picks nothing.  Written in ascending order, -1 behind the last.  Sums and products are held in 64 bits, so that
+ * the lists do not depend on the order of sums.  Of the problem, topk, dtype, maps, regions, strides and sizes count.
+ */
+int slide_region_select(const slide_region_problem* p, const void* q, const void* k, int* index,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * out[row] = sum over the keys n of the row's listed regions of keep_n P_n v_n,  P = softmax(scale q.k),
+ * keep_n as `dropout` says.  lse: float32 [B, heads, q_h, q_w] or NULL: log sum exp(scale q.k), which the backward takes.
+ */
+int slide_region_attn_fwd(const slide_region_problem* p, const void* q, const void* k, const void* v, const int* index,
+                          void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of slide_region_attn_fwd (none through the lists): dq [B, q_h, q_w, heads * head_dim], dk and dv
+ * [B, k_h, k_w, kv_heads * head_dim], overwritten, zeros where nothing arrives.  out and lse are the forward's results.  With an
+ * image stride of 0 the gradients are still those of every image.
+ */
+int slide_region_attn_bwd(const slide_region_problem* p, const void* dout, const void* q, const void* k, const void* v,
+                          const int* index, const void* out, const float* lse, void* dq, void* dk, void* dv,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout of n contiguous elements of `dtype`, with the residual of the block added on the way:
+ *     y[i] = residual[i] + keep(i) x[i]         (residual may be NULL; y may be x or residual)
+ *     dx[i] = keep(i) dout[i]                   (the residual's gradient is dout itself; dx may be dout)
+ * keep(i) is 65536 / (65536 - t), t = p rounded to 65536ths, where half word i % 8 of Philox-4x32-7 with key seed and counter
+ * (low 32 bits of i / 8, high 32 bits of i / 8 with the top bit set, 2^32 - 1, offset) is at least t, and 0 elsewhere (a dropped
+ * element contributes nothing, whatever it holds).  p, seed, offset, offset_device as for the attention weights of
+ * slide_region_problem; the two draw from disjoint counters.  The mask is never stored.  1 <= n < 2^48.
+ */
+int slide_dropout_fwd(const void* x, const void* residual, void* y, long long n, int dtype, float p,
+                      unsigned long long seed, unsigned int offset, const long long* offset_device, void* stream);
+int slide_dropout_bwd(const void* dout, void* dx, long long n, int dtype, float p,
+                      unsigned long long seed, unsigned int offset, const long long* offset_device, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,4 +1,5 @@
-"""MI355X-native Slide Attention operator (arxiv 2304.04237, Sec. 4).
+"""MI355X-native Slide Attention operator (arxiv 2304.04237, Sec. 4), and next to it attention over selected regions
+and dropout for the stages of a backbone where a window is too little.
 
 A thin binding over libslide_attn.so (hand-written gfx950 HIP kernels behind a
 C ABI, see include/slide_attn.h).  PyTorch is used for device memory and streams
@@ -24,4 +25,12 @@ from .binding import (  # noqa: F401
     slide_attn_workspace_bytes,
     slide_reparam,
     slide_status_string,
+)
+from .region import (  # noqa: F401
+    slide_dropout_bwd,
+    slide_dropout_fwd,
+    slide_region_attn_bwd,
+    slide_region_attn_fwd,
+    slide_region_select,
+    slide_region_workspace_bytes,
 )

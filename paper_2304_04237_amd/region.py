@@ -1,0 +1,273 @@
+"""ctypes binding of region selection, region attention and dropout: argument marshalling only.
+
+Function names match the C ABI (include/slide_attn.h, which has the definitions).  Activations are float32 or bfloat16 tensors
+[B, H, W, heads * head_dim], channels last; q, k and v may be parts of a wider tensor (a slice of the channels of one
+projection's output, the first columns of a longer cache) as long as the channels of a pixel are contiguous and the pixels of an
+image evenly spaced in raster order.  A sequence [B, n, C] is passed as a map of height 1.  Work is enqueued on torch's current
+stream of the tensors' device.
+"""
+import ctypes
+
+import torch
+
+from .binding import SLIDE_BF16, SLIDE_F32, SlideAttnError, _check, _stream, load_library
+
+_vp = ctypes.c_void_p
+_SELECT, _FWD, _BWD = 0, 1, 2
+
+
+class _Problem(ctypes.Structure):
+    """slide_region_problem."""
+    _fields_ = [(n, ctypes.c_int) for n in ("B", "heads", "kv_heads", "head_dim", "q_h", "q_w", "k_h", "k_w", "q_region_h",
+                                            "q_region_w", "k_region_h", "k_region_w", "topk", "dtype")] + \
+               [(n, ctypes.c_longlong) for n in ("q_pixel", "q_image", "k_pixel", "k_image", "v_pixel", "v_image")] + \
+               [("q_size", _vp), ("k_size", _vp), ("scale", ctypes.c_float), ("dropout", ctypes.c_float),
+                ("seed", ctypes.c_ulonglong), ("offset", ctypes.c_uint), ("offset_device", _vp)]
+
+
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = load_library()
+        i, sz, u64, u32, ll = ctypes.c_int, ctypes.c_size_t, ctypes.c_ulonglong, ctypes.c_uint, ctypes.c_longlong
+        p = ctypes.POINTER(_Problem)
+        lib.slide_region_workspace_bytes.restype = sz
+        lib.slide_region_workspace_bytes.argtypes = [p, i]
+        lib.slide_region_select.restype = i
+        lib.slide_region_select.argtypes = [p] + [_vp] * 4 + [sz, _vp]
+        lib.slide_region_attn_fwd.restype = i
+        lib.slide_region_attn_fwd.argtypes = [p] + [_vp] * 7 + [sz, _vp]
+        lib.slide_region_attn_bwd.restype = i
+        lib.slide_region_attn_bwd.argtypes = [p] + [_vp] * 11 + [sz, _vp]
+        lib.slide_dropout_fwd.restype = i
+        lib.slide_dropout_fwd.argtypes = [_vp] * 3 + [ll, i, ctypes.c_float, u64, u32, _vp, _vp]
+        lib.slide_dropout_bwd.restype = i
+        lib.slide_dropout_bwd.argtypes = [_vp] * 2 + [ll, i, ctypes.c_float, u64, u32, _vp, _vp]
+        _lib = lib
+    return _lib
+
+
+_CODES = {torch.float32: SLIDE_F32, torch.bfloat16: SLIDE_BF16}
+
+
+def _code(t):
+    if t.dtype not in _CODES:
+        raise SlideAttnError("activations must be float32 or bfloat16, got %s" % t.dtype)
+    return _CODES[t.dtype]
+
+
+def _int(value, name, lo, hi):
+    if isinstance(value, bool) or not hasattr(value, "__index__") or not lo <= value.__index__() <= hi:
+        raise SlideAttnError("%s must be an integer in [%d, %d]" % (name, lo, hi))
+    return value.__index__()
+
+
+def _strides(t, name):
+    """Elements between the pixels and between the images of a [B, H, W, C] tensor."""
+    B, H, W, C = t.shape
+    sb, sh, sw, sc = t.stride()
+    if W == 1:                                  # (strides of single elements say nothing)
+        sw = sh if H > 1 else C
+    if (C > 1 and sc != 1) or (H > 1 and sh != W * sw):
+        raise SlideAttnError("%s must have contiguous channels and evenly spaced pixels" % name)
+    return sw, (sb if B > 1 else 0)
+
+
+def _on(t, name, device):
+    if not t.is_cuda:
+        raise SlideAttnError("%s must live on the GPU" % name)
+    if t.device != device:
+        raise SlideAttnError("%s must live on the device of the first argument" % name)
+
+
+def _like(t, name, shape, dtype, device):
+    """A tensor that must have this shape and type, and be contiguous."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise SlideAttnError("%s must be %s %s" % (name, str(dtype)[6:], list(shape)))
+    _on(t, name, device)
+    if not t.is_contiguous():
+        raise SlideAttnError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _random(p, dropout, seed, offset, device):
+    if not 0.0 <= dropout < 1.0 - 2.0 ** -17:
+        raise SlideAttnError("dropout must be in [0, 1 - 2^-17)")
+    number, holder = (0, offset) if isinstance(offset, torch.Tensor) else (_int(offset, "offset", 0, 2 ** 32 - 1), None)
+    if holder is not None:
+        if holder.dtype != torch.int64 or holder.numel() != 1:
+            raise SlideAttnError("offset must be an integer or an int64 tensor with one element")
+        _on(holder, "offset", device)
+    return float(dropout), _int(seed, "seed", 0, 2 ** 64 - 1), number, None if holder is None else holder.data_ptr()
+
+
+def _problem(q, maps, heads, q_region, k_region, kv_heads, topk, q_size, k_size):
+    """The problem of maps q, k (and v), with everything checked that a kernel relies on."""
+    p = _Problem()
+    if q.dim() != 4:
+        raise SlideAttnError("activations must be [B, H, W, C]")
+    p.dtype = _code(q)
+    _on(q, "q", q.device)
+    p.B, p.q_h, p.q_w, channels = q.shape
+    p.heads = _int(heads, "heads", 1, 65535)
+    p.kv_heads = p.heads if kv_heads is None else _int(kv_heads, "kv_heads", 1, 65535)
+    if p.heads % p.kv_heads or channels % p.heads:
+        raise SlideAttnError("channels must be a multiple of heads, and heads of kv_heads")
+    p.head_dim = channels // p.heads
+    if not 1 <= p.head_dim <= 128:
+        raise SlideAttnError("head size must be 1..128")
+    shape = None
+    for name, t in maps:
+        if t.dim() != 4 or t.dtype != q.dtype or t.shape[0] != p.B or t.shape[3] != p.kv_heads * p.head_dim \
+                or t.shape != (shape or t.shape):
+            raise SlideAttnError("%s must be %s [%d, H, W, %d]%s" % (name, str(q.dtype)[6:], p.B, p.kv_heads * p.head_dim,
+                                                                   "" if shape is None else " as k is"))
+        shape = t.shape
+        _on(t, name, q.device)
+    p.k_h, p.k_w = shape[1], shape[2]
+    if min(p.B, p.q_h, p.q_w, p.k_h, p.k_w) < 1:
+        raise SlideAttnError("maps must not be empty")
+    p.q_pixel, p.q_image = _strides(q, "q")
+    p.k_pixel, p.k_image = _strides(maps[0][1], "k")
+    p.v_pixel, p.v_image = _strides(maps[1][1], "v") if len(maps) > 1 else (0, 0)
+    for name, region in (("q_region", q_region), ("k_region", k_region)):
+        if len(region) != 2:
+            raise SlideAttnError("%s must be (height, width)" % name)
+    p.q_region_h, p.q_region_w = (_int(n, "q_region", 1, 2 ** 31 - 1) for n in q_region)
+    p.k_region_h, p.k_region_w = (_int(n, "k_region", 1, 2 ** 31 - 1) for n in k_region)
+    p.topk = _int(topk, "topk", 1, 1024)
+    p.q_size = None if q_size is None else _like(q_size, "q_size", (p.B, 2), torch.int32, q.device)
+    p.k_size = None if k_size is None else _like(k_size, "k_size", (p.B, 2), torch.int32, q.device)
+    return p
+
+
+def _groups(p):
+    return -(-p.q_h // p.q_region_h) * -(-p.q_w // p.q_region_w)
+
+
+class _On:
+    """The device of a call made current where it is not."""
+
+    def __init__(self, device):
+        self.index, self.guard = device.index, None
+        if torch.cuda.current_device() != self.index:
+            self.guard = torch.cuda.device(self.index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return _stream(self.index)
+
+    def __exit__(self, *error):
+        if self.guard is not None:
+            self.guard.__exit__(*error)
+
+
+def _workspace(lib, p, call, workspace, like):
+    """Pointer and bytes of the scratch: the caller's, or as much as the call needs."""
+    if workspace is None:
+        need = lib.slide_region_workspace_bytes(p, call)
+        if need == 0:
+            return None, 0, None
+        workspace = like.new_empty((need,), dtype=torch.uint8)
+    else:
+        _on(workspace, "workspace", like.device)
+        if not workspace.is_contiguous():
+            raise SlideAttnError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def slide_region_workspace_bytes(call, q, k, topk, heads, q_region, k_region, kv_heads=None):
+    """Bytes of scratch of slide_region_select ("select"), slide_region_attn_fwd ("fwd") or slide_region_attn_bwd ("bwd")."""
+    p = _problem(q, (("k", k), ("v", k)), heads, q_region, k_region, kv_heads, topk, None, None)
+    with _On(q.device):
+        return int(_library().slide_region_workspace_bytes(p, {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call]))
+
+
+def slide_region_select(q, k, topk, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None, index=None, workspace=None):
+    """The lists: int32 [B, kv_heads, regions of q, topk], ascending, -1 behind the last.
+
+    q_size, k_size: int32 [B, 2] tensors, the valid height and width of every image (None: the whole map)."""
+    lib = _library()
+    p = _problem(q, (("k", k),), heads, q_region, k_region, kv_heads, topk, q_size, k_size)
+    shape = (p.B, p.kv_heads, _groups(p), p.topk)
+    with _On(q.device) as stream:
+        if index is None:
+            index = q.new_empty(shape, dtype=torch.int32)
+        ws, size, keep = _workspace(lib, p, _SELECT, workspace, q)
+        _check(lib.slide_region_select(p, q.data_ptr(), k.data_ptr(), _like(index, "index", shape, torch.int32, q.device), ws, size, stream))
+    return index
+
+
+def _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset):
+    if index.dim() != 4:
+        raise SlideAttnError("index must be int32 [B, kv_heads, regions of q, topk]")
+    p = _problem(q, (("k", k), ("v", v)), heads, q_region, k_region, kv_heads, index.shape[3], q_size, k_size)
+    p.dropout, p.seed, p.offset, p.offset_device = _random(p, dropout, seed, offset, q.device)
+    if scale is not None and not 0.0 < scale < float("inf"):
+        raise SlideAttnError("scale must be positive")
+    p.scale = 0.0 if scale is None else scale
+    return p, _like(index, "index", (p.B, p.kv_heads, _groups(p), p.topk), torch.int32, q.device)
+
+
+def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None, scale=None,
+                          dropout=0.0, seed=0, offset=0, out=None, lse=None, workspace=None):
+    """out: every row of q over the keys of its region's list.  lse: optional float32 [B, heads, H, W] tensor that receives
+    the log of the softmax denominators (the backward takes it).
+
+    dropout, seed, offset: of the attention weights; offset may be an int64 tensor with one element, read when the kernels run."""
+    lib = _library()
+    p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
+    with _On(q.device) as stream:
+        out = q.new_empty(q.shape) if out is None else out
+        out_at = _like(out, "out", q.shape, q.dtype, q.device)
+        lse_at = None if lse is None else _like(lse, "lse", (p.B, p.heads, p.q_h, p.q_w), torch.float32, q.device)
+        ws, size, keep = _workspace(lib, p, _FWD, workspace, q)
+        _check(lib.slide_region_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, out_at, lse_at, ws, size, stream))
+    return out
+
+
+def slide_region_attn_bwd(dout, q, k, v, index, out, lse, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None,
+                          scale=None, dropout=0.0, seed=0, offset=0, outputs=None, workspace=None):
+    """Returns (dq, dk, dv), contiguous.  out, lse: the forward's results for the same arguments."""
+    lib = _library()
+    p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
+    with _On(q.device) as stream:
+        dq, dk, dv = (q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)) if outputs is None else outputs
+        at = [_like(t, name, like.shape, q.dtype, q.device)
+              for t, name, like in ((dout, "dout", q), (out, "out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
+        lse_at = _like(lse, "lse", (p.B, p.heads, p.q_h, p.q_w), torch.float32, q.device)
+        ws, size, keep = _workspace(lib, p, _BWD, workspace, q)
+        _check(lib.slide_region_attn_bwd(p, at[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, at[1], lse_at, *at[2:], ws, size, stream))
+    return dq, dk, dv
+
+
+def _dropout(entry, x, name, residual, p, seed, offset, y):
+    if not x.is_cuda:
+        raise SlideAttnError("%s must live on the GPU" % name)
+    if not x.is_contiguous():
+        raise SlideAttnError("%s must be contiguous" % name)
+    code = _code(x)
+    p, seed, number, holder = _random(None, p, seed, offset, x.device)
+    with _On(x.device) as stream:
+        y = x.new_empty(x.shape) if y is None else y
+        y_at = _like(y, "the result", x.shape, x.dtype, x.device)
+        at = (x.data_ptr(),)
+        if residual is not False:
+            at += (None if residual is None else _like(residual, "residual", x.shape, x.dtype, x.device),)
+        if x.numel():
+            _check(entry(*at, y_at, x.numel(), code, p, seed, number, holder, stream))
+    return y
+
+
+def slide_dropout_fwd(x, p, seed, offset=0, residual=None, out=None):
+    """residual + dropout(x) of any contiguous tensor; the mask follows from seed, offset and the element's number."""
+    return _dropout(_library().slide_dropout_fwd, x, "x", residual, p, seed, offset, out)
+
+
+def slide_dropout_bwd(dout, p, seed, offset=0, dx=None):
+    """The gradient of x (the residual's is dout itself), with the mask of the forward's p, seed and offset."""
+    return _dropout(_library().slide_dropout_bwd, dout, "dout", False, p, seed, offset, dx)
