@@ -11,6 +11,19 @@
 namespace slide {
 namespace region {
 
+// Division of numbers below 2^31 by a number that the host knows: one product.  (n m) >> (31 + s) with m = floor(2^(31 + s) / x) + 1,
+// s = ceil(log2 x), is exact for n < 2^31: m x exceeds 2^(31 + s) by at most x <= 2^s.
+struct Div {
+    uint32_t x, m, s;
+    __host__ static Div by(uint32_t x)
+    {
+        uint32_t s = 0;
+        while ((1ull << s) < x) ++s;
+        return Div{x, (uint32_t)((1ull << (31 + s)) / x + 1), s};
+    }
+    __device__ __forceinline__ int of(int n) const { return (int)(__umulhi((uint32_t)n << 1, m) >> s); }
+};
+
 // A map of pixels cut into regions: what the kernels need to find a pixel.
 struct Map {
     int H, W;               // pixels
@@ -18,6 +31,7 @@ struct Map {
     int across, regions;    // regions side by side, and in all
     int places;             // h * w
     const int* size;        // [B][2] valid height and width of each image, or null
+    Div by_across, by_w;
     // valid height and width of image b, within the map
     __device__ __forceinline__ void limits(int b, int& vh, int& vw) const
     {
@@ -27,8 +41,8 @@ struct Map {
     // pixel at `place` of region `r`, or -1 outside (vh, vw)
     __device__ __forceinline__ int pixel(int r, int place, int vh, int vw) const
     {
-        const int ry = r / across, rx = r - ry * across;
-        const int py = place / w, px = place - py * w;
+        const int ry = by_across.of(r), rx = r - ry * across;
+        const int py = by_w.of(place), px = place - py * w;
         const int y = ry * h + py, x = rx * w + px;
         return y < vh && x < vw ? y * W + x : -1;
     }
@@ -69,6 +83,7 @@ struct Args {
     int B, heads, kv, g, d, T, dtype;
     int R;                              // rows of a group
     int quads, pairs;                   // ceil(key places / 4), ceil(R / 2): the dropout counter counts patches of 4 keys and 2 rows
+    Div by_g, by_slots;                 // slots: 4 * quads, what a listed region takes in a group's row of keys
     Map qm, km;
     Strides qs, ks, vs;
     float scale;

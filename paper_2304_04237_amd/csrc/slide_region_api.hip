@@ -13,7 +13,7 @@ static bool make_map(int H, int W, int h, int w, const int* size, slide::region:
     if ((long long)H * W >= 1ll << 29) return false;                    // (regions * places stay below 2^31)
     h = std::min(h, H); w = std::min(w, W);
     const int across = (W + w - 1) / w, down = (H + h - 1) / h;
-    m = slide::region::Map{H, W, h, w, across, across * down, h * w, size};
+    m = slide::region::Map{H, W, h, w, across, across * down, h * w, size, slide::region::Div::by(across), slide::region::Div::by(w)};
     return (long long)across * down * h * w < 1ll << 31;
 }
 
@@ -50,6 +50,11 @@ static int check(const slide_region_problem* p, int call, Args& a)
     if (rows * a.qm.regions >= 1ll << 31) return SLIDE_ERR_SHAPE;       // (the dropout counter's second word)
     a.R = (int)rows;
     a.quads = (a.km.places + 3) / 4; a.pairs = (a.R + 1) / 2;
+    a.by_g = slide::region::Div::by(a.g); a.by_slots = slide::region::Div::by(4 * a.quads);
+    if (4ll * a.quads * a.T >= (1ll << 31) - 256) return SLIDE_ERR_SHAPE;        // (slots of a group, and some past its end)
+    // waves of one launch: every 32 rows of a group, every 32 places of a region of keys
+    if ((long long)a.B * a.kv * a.qm.regions * ((a.R + 31) / 32) >= 1ll << 26 ||
+        (long long)a.B * a.kv * a.km.regions * ((a.km.places + 31) / 32) >= 1ll << 26) return SLIDE_ERR_SHAPE;
     if ((long long)a.quads * a.km.regions >= 1ll << 32) return SLIDE_ERR_SHAPE;
     if ((long long)a.qm.regions * a.T >= 1ll << 31) return SLIDE_ERR_SHAPE;
     if (!strides_fit(p->q_pixel, p->q_image, p->heads * p->head_dim, a.qm) || !strides_fit(p->k_pixel, p->k_image, p->kv_heads * p->head_dim, a.km))

@@ -137,16 +137,6 @@ __global__ __launch_bounds__(64) void key_kernel(Args a, const void* dout, const
     store_row<T>(dv, k_at, a.d, lane, gv);
 }
 
-size_t fwd_workspace_bytes(const Args&) { return 0; }
-
-hipError_t launch_fwd(const Args& a, void* out, float* lse, void*, hipStream_t st)
-{
-    const dim3 grid(a.R, a.qm.regions, a.B * a.kv);
-    if (a.dtype == 0) row_kernel<float, false><<<grid, 64, 0, st>>>(a, nullptr, out, lse, nullptr, nullptr);
-    else row_kernel<bf16_bits, false><<<grid, 64, 0, st>>>(a, nullptr, out, lse, nullptr, nullptr);
-    return hipGetLastError();
-}
-
 size_t bwd_workspace_bytes(const Args& a) { return (size_t)a.B * a.heads * a.qm.H * a.qm.W * sizeof(float); }
 
 hipError_t launch_bwd(const Args& a, const void* dout, const void* out, const float* lse, void* dq, void* dk, void* dv,

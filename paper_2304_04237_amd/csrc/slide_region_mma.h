@@ -1,0 +1,220 @@
+// Pieces of the matrix-core kernels of region attention (slide_region_fwd.hip, slide_region_bwd.hip).
+//
+// Tiles are 32 x 32.  bf16: v_mfma_f32_32x32x16_bf16, a lane holding 8 consecutive elements of the contracted axis; float32:
+// v_mfma_f32_32x32x2_f32, a lane holding one.  A product's result has column lane % 32 and, in register r, row
+// 8 (r / 4) + 4 (lane / 32) + r % 4.  A result that becomes the right operand of the next product (weights, logit gradients) stays in
+// its registers: the contracted axis may be numbered as one likes as long as the left operand follows, so slot e of a lane in
+// step t is the row that register 8 t + e holds.  The left operand of that product is the transpose of a staged tile
+// (keys x channels): bf16 by the transposing LDS read, float32 by reading a column.
+#pragma once
+#include "slide_region.h"
+
+namespace slide {
+namespace region {
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+// row that register r of a product's result is in lane half h
+__device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// The registers of an operand with D contracted channels (or 32 contracted rows), per lane
+template <typename T, int D> struct Operand;
+template <int D> struct Operand<bf16_bits, D> { u4 v[D / 16]; };
+template <int D> struct Operand<float, D> { f4 v[D / 8]; };
+
+// Memory piece i (16 bytes) of an operand's lane half h starts at this channel
+template <typename T, int D> __device__ __forceinline__ constexpr int piece_channel(int i, int h)
+{
+    return sizeof(T) == 2 ? 16 * i + 8 * h : h * (D / 2) + 4 * i;
+}
+
+// One 16-byte piece of a pixel's channels, zeros beyond `left` channels.  vec: the pieces are whole and 16-byte aligned.
+__device__ __forceinline__ u4 load_piece(const bf16_bits* p, int left, bool vec)
+{
+    u4 x = {0, 0, 0, 0};
+    if (vec) {
+        if (left > 0) x = *(const u4*)p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) x[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    }
+    return x;
+}
+__device__ __forceinline__ f4 load_piece(const float* p, int left, bool vec)
+{
+    f4 x = {0, 0, 0, 0};
+    if (vec) {
+        if (left > 0) x = *(const f4*)p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) x[e] = p[e];
+    }
+    return x;
+}
+
+// The operand whose lane is one pixel's channels at p; zeros where the pixel does not count
+template <typename T, int D>
+__device__ __forceinline__ void load_operand(Operand<T, D>& o, const T* p, bool ok, int d, int h, bool vec)
+{
+    constexpr int N = sizeof(T) == 2 ? D / 16 : D / 8;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = piece_channel<T, D>(i, h);
+        o.v[i] = load_piece(p + c, ok ? d - c : 0, vec);
+    }
+}
+
+// acc += A^T B over the D channels of two operands (rows: A's lanes, columns: B's lanes)
+template <int D>
+__device__ __forceinline__ f16v dot(const Operand<bf16_bits, D>& a, const Operand<bf16_bits, D>& b, f16v acc)
+{
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a.v[i]), __builtin_bit_cast(bf8, b.v[i]), acc, 0, 0, 0);
+    return acc;
+}
+template <int D>
+__device__ __forceinline__ f16v dot(const Operand<float, D>& a, const Operand<float, D>& b, f16v acc)
+{
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i >> 2][i & 3], b.v[i >> 2][i & 3], acc, 0, 0, 0);
+    return acc;
+}
+
+// A tile of 32 pixels x D channels in LDS that this wave alone uses
+template <typename T, int D> struct Tile {
+    static constexpr int BYTES = 32 * D * (int)sizeof(T);
+};
+
+// the pieces of a lane (pixel lane % 32, half of the pieces) into the tile
+template <int D>
+__device__ __forceinline__ void stage(unsigned char* tile, const Operand<bf16_bits, D>& o, int lane)
+{
+    const int row = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) *(u4*)(tile + row * D * 2 + (2 * i + h) * 16) = o.v[i];
+}
+template <int D>
+__device__ __forceinline__ void stage(unsigned char* tile, const Operand<float, D>& o, int lane)
+{
+    const int row = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) *(f4*)(tile + (row * D + h * (D / 2) + 4 * i) * 4) = o.v[i];
+}
+
+// Weights of 32 rows (registers of a product's result) as a right operand
+template <typename T> struct Weights;
+template <> struct Weights<bf16_bits> {
+    u4 v[2];
+    // rounded to bf16 (to nearest): the products take no more
+    __device__ __forceinline__ void set(const f16v& p)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = (uint32_t)f32_to_bf16(p[2 * i]) | (uint32_t)f32_to_bf16(p[2 * i + 1]) << 16;
+    }
+};
+template <> struct Weights<float> {
+    f16v v;
+    __device__ __forceinline__ void set(const f16v& p) { v = p; }
+};
+
+// The transpose of channels 32 dt .. 32 dt + 31 of a tile as a left operand, rows numbered as Weights' slots
+template <int D>
+__device__ __forceinline__ void read_transposed(u4 (&a)[2], const unsigned char* tile, int dt, int lane)
+{
+    const int s = lane & 15, h = lane >> 5, dh = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned char* p = tile + (8 * i + 4 * h + (s >> 2)) * D * 2 + (32 * dt + 16 * dh + 4 * (s & 3)) * 2;
+        const u2 x = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)p));
+        a[i >> 1][2 * (i & 1)] = x[0];
+        a[i >> 1][2 * (i & 1) + 1] = x[1];
+    }
+}
+
+// acc[dt] += (channels x rows of the tile) (rows x columns of w), for NC sets of columns
+template <int D, int NC>
+__device__ __forceinline__ void accumulate(f16v (&acc)[NC][D / 32], const unsigned char* tile, const Weights<bf16_bits> (&w)[NC], int lane)
+{
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) {
+        u4 a[2];
+        read_transposed<D>(a, tile, dt, lane);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                acc[c][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a[t]), __builtin_bit_cast(bf8, w[c].v[t]), acc[c][dt], 0, 0, 0);
+    }
+}
+template <int D, int NC>
+__device__ __forceinline__ void accumulate(f16v (&acc)[NC][D / 32], const unsigned char* tile, const Weights<float> (&w)[NC], int lane)
+{
+    const float* t = (const float*)tile + (lane & 31);
+    const int h = lane >> 5;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float a = t[acc_row(r, h) * D + 32 * dt];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) acc[c][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[c].v[r], acc[c][dt], 0, 0, 0);
+        }
+}
+
+// LDS operations of a wave run in order; this keeps the compiler from moving them past each other
+__device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
+
+// the larger, the sum, of the two lane halves' values
+__device__ __forceinline__ float halves_max(float x)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float halves_sum(float x)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// four consecutive channels c .. c + 3 of a pixel
+__device__ __forceinline__ void store4(bf16_bits* p, const float (&x)[4], int left, bool vec)
+{
+    if (vec) {
+        if (left > 0)
+            *(u2*)p = u2{(uint32_t)f32_to_bf16(x[0]) | (uint32_t)f32_to_bf16(x[1]) << 16, (uint32_t)f32_to_bf16(x[2]) | (uint32_t)f32_to_bf16(x[3]) << 16};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = f32_to_bf16(x[e]);
+    }
+}
+__device__ __forceinline__ void store4(float* p, const float (&x)[4], int left, bool vec)
+{
+    if (vec) {
+        if (left > 0) *(f4*)p = f4{x[0], x[1], x[2], x[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = x[e];
+    }
+}
+
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: work items that share keys are given to one XCD in a row.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t block, uint32_t blocks)
+{
+    const uint32_t whole = blocks & ~7u;
+    return block < whole ? (block & 7) * (whole >> 3) + (block >> 3) : block;
+}
+
+}  // namespace region
+}  // namespace slide
