@@ -330,8 +330,9 @@ int slide_attn_fwd_traffic_probe(const void* q, const void* k, const void* v, vo
  * is at least t (half word 2 w + 1 is the upper half of word w).  offset: the number of the call, plus the low 32 bits of what
  * offset_device (one integer on the device, or NULL) holds when the kernels run: a captured graph draws new masks with it.
  *
- * Limits: head_dim 1..128, topk 1..1024, fewer than 2^29 pixels per map, fewer than 2^26 times 32 rows (rows of a region counted
- * up to a multiple of 32) over all regions, key heads and images, and as many places of key regions likewise;
+ * Limits: head_dim 1..128, topk 1..1024, fewer than 2^29 pixels per map, fewer than 2^24 times 32 rows (rows of a region counted
+ * up to a multiple of 32) over all regions, key heads and images, as many places of key regions likewise, and fewer than 2^30
+ * entries in the lists of an image's key head;
  * slide_region_select: at most 16384 regions of keys.
  * SLIDE_ERR_SHAPE otherwise, and for a dropout outside [0, 1) or one that rounds to 1, a negative or NaN scale, and strides that
  * let pixels of one map overlap.  Products are formed from the activations as they are (bf16: exactly), sums and softmax

@@ -96,7 +96,7 @@ struct Args {
 size_t select_workspace_bytes(const Args& a);
 hipError_t launch_select(const Args& a, int* index, void* workspace, hipStream_t st);
 
-// ---- region attention (slide_region_attn.hip)
+// ---- region attention (slide_region_fwd.hip, slide_region_bwd.hip)
 size_t fwd_workspace_bytes(const Args& a);
 hipError_t launch_fwd(const Args& a, void* out, float* lse, void* workspace, hipStream_t st);
 size_t bwd_workspace_bytes(const Args& a);

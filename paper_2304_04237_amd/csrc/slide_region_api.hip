@@ -53,10 +53,10 @@ static int check(const slide_region_problem* p, int call, Args& a)
     a.by_g = slide::region::Div::by(a.g); a.by_slots = slide::region::Div::by(4 * a.quads);
     if (4ll * a.quads * a.T >= (1ll << 31) - 256) return SLIDE_ERR_SHAPE;        // (slots of a group, and some past its end)
     // waves of one launch: every 32 rows of a group, every 32 places of a region of keys
-    if ((long long)a.B * a.kv * a.qm.regions * ((a.R + 31) / 32) >= 1ll << 26 ||
-        (long long)a.B * a.kv * a.km.regions * ((a.km.places + 31) / 32) >= 1ll << 26) return SLIDE_ERR_SHAPE;
+    if ((long long)a.B * a.kv * a.qm.regions * ((a.R + 31) / 32) >= 1ll << 24 ||
+        (long long)a.B * a.kv * a.km.regions * ((a.km.places + 31) / 32) >= 1ll << 24) return SLIDE_ERR_SHAPE;
     if ((long long)a.quads * a.km.regions >= 1ll << 32) return SLIDE_ERR_SHAPE;
-    if ((long long)a.qm.regions * a.T >= 1ll << 31) return SLIDE_ERR_SHAPE;
+    if ((long long)a.qm.regions * a.T >= 1ll << 30) return SLIDE_ERR_SHAPE;
     if (!strides_fit(p->q_pixel, p->q_image, p->heads * p->head_dim, a.qm) || !strides_fit(p->k_pixel, p->k_image, p->kv_heads * p->head_dim, a.km))
         return SLIDE_ERR_SHAPE;
     if (call == SLIDE_REGION_SELECT) {

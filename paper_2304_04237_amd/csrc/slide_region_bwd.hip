@@ -1,0 +1,564 @@
+// Region attention, backward, on the matrix cores.
+//
+//   P = exp(S - lse);  D = dout.out;  dS = P (F dP - D),  dP = dout.v,  F the weights' dropout factors
+//   dq = scale sum dS k   (row kernel: a wave per 32 NR rows of a group, over the group's keys, like the forward)
+//   dk = scale sum dS q,  dv = sum F P dout   (key kernel: a wave per 32 NK keys of a region, over the rows of the groups that list it)
+//
+// Between the two a kernel turns the lists around (which groups list region j, in ascending order, so that sums have one order).
+// A wave takes at most `share` of a region's groups; what is beyond goes to further waves, whose float32 sums a last kernel adds up.
+#include "slide_region_mma.h"
+
+namespace slide {
+namespace region {
+
+struct BwdArgs {
+    Args a;
+    const void* dout;
+    const void* out;
+    const float* lse;
+    void* dq;
+    void* dk;
+    void* dv;
+    float* row_lse;         // [groups][row_tiles * 32]: lse in units of log 2, +infinity for a row that takes no part
+    float* row_D;
+    int2* sorted;           // [B * kv][regions of q * T]: (group, region) of every entry that counts, by region, then by group
+    int* start;             // [B * kv][J + 1]
+    float* partial;         // [B * kv][key tiles][2 windows][2][32 NK][D]
+    int slots, tiles, row_tiles, key_tiles, items;
+    int entries;            // regions of q * T
+    int share, windows;     // entries per wave, ceil(entries / share)
+    Div by_row_tiles;
+    int vec_q, vec_k, vec_v, vec_do, vec_o, vec_dq, vec_dk;
+};
+
+template <typename T> __device__ __forceinline__ float piece_dot(const u4& a, const u4& b);
+template <> __device__ __forceinline__ float piece_dot<bf16_bits>(const u4& a, const u4& b)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        s = __builtin_fmaf(__uint_as_float(a[e] << 16), __uint_as_float(b[e] << 16), s);
+        s = __builtin_fmaf(__uint_as_float(a[e] & 0xffff0000u), __uint_as_float(b[e] & 0xffff0000u), s);
+    }
+    return s;
+}
+template <> __device__ __forceinline__ float piece_dot<float>(const u4& a, const u4& b)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = __builtin_fmaf(__uint_as_float(a[e]), __uint_as_float(b[e]), s);
+    return s;
+}
+
+// dq and, for the key kernel, every row's lse and D.
+// bf16: out was rounded, so dout.out is off by up to 2^-8 of its terms.  The sum of P F dP, which is D without that, is only known at
+// the end; until then the rounded D0 is used, and dq is corrected by (D - D0) sum P k, for one more product.
+template <typename T, int D, int NR, bool DROP>
+__global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
+{
+    constexpr bool FIX = sizeof(T) == 2;
+    const Args& a = f.a;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int item = (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
+    if (item >= f.items) return;
+    unsigned char* tile = lds + wave * Tile<T, D>::BYTES;
+    const int group = item / f.tiles, row0 = (item - group * f.tiles) * 32 * NR;
+    const int bm = group / a.qm.regions, i = group - bm * a.qm.regions;
+    const int b = bm / a.kv, m = bm - b * a.kv;
+    const int col = lane & 31, h = lane >> 5;
+
+    Operand<T, D> q[NR], g[NR];
+    long long out_at[NR];
+    float row_lse[NR], D0[NR], D1[NR];
+    {
+        int vh, vw;
+        a.qm.limits(b, vh, vw);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const int r = row0 + 32 * n + col;
+            const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
+            const int px = r < a.R ? a.qm.pixel(i, place, a.qm.H, a.qm.W) : -1;
+            const bool ok = r < a.R && a.qm.pixel(i, place, vh, vw) >= 0;
+            const long long n_px = (long long)a.qm.H * a.qm.W;
+            out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
+            const long long at = ok ? out_at[n] : 0;
+            load_operand<T, D>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h, f.vec_q);
+            load_operand<T, D>(g[n], (const T*)f.dout + at, ok, a.d, h, f.vec_do);
+            Operand<T, D> o;
+            load_operand<T, D>(o, (const T*)f.out + at, ok, a.d, h, f.vec_o);
+            float s = 0.0f;
+#pragma unroll
+            for (int u = 0; u < (int)(sizeof(o) / 16); ++u)
+                s += piece_dot<T>(__builtin_bit_cast(u4, o.v[u]), __builtin_bit_cast(u4, g[n].v[u]));
+            D0[n] = halves_sum(s);
+            D1[n] = 0.0f;
+            const float l = ok ? f.lse[((long long)b * a.heads + head) * n_px + px] : -INFINITY;
+            row_lse[n] = l == -INFINITY ? INFINITY : l * LOG2E;
+        }
+    }
+    const uint32_t call = DROP ? a.rnd.call() : 0;
+    const float c2 = a.scale * LOG2E, keep = DROP ? a.rnd.scale : 1.0f;
+    constexpr int NA = FIX ? 2 * NR : NR;
+    f16v acc[NA][D / 32];           // sums of dS k, then of P k
+#pragma unroll
+    for (int n = 0; n < NA; ++n)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) acc[n][dt] = f16v{};
+
+    const T* kp = (const T*)a.k + b * a.ks.image + m * a.d;
+    const T* vp = (const T*)a.v + b * a.vs.image + m * a.d;
+    Walk walk;
+    walk.list = a.index + (long long)group * a.T;
+    a.km.limits(b, walk.vh, walk.vw);
+    Operand<T, D> kn, vn;
+    int region = walk.look(a, col, f.slots);
+    uint32_t next_word = 0, next_ok;
+    auto fetch = [&]() {
+        const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
+        next_ok = (uint32_t)__ballot(px >= 0);
+        if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
+        load_operand<T, D>(kn, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h, f.vec_k);
+        load_operand<T, D>(vn, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h, f.vec_v);
+    };
+    fetch();
+    region = walk.look(a, 32 + col, f.slots);
+    for (int x = 0; x < f.slots; x += 32) {
+        const Operand<T, D> k = kn, v = vn;
+        const uint32_t ok = next_ok, word = next_word;
+        wave_order();
+        stage<D>(tile, k, lane);
+        wave_order();
+        if (x + 32 < f.slots) {
+            fetch();
+            region = walk.look(a, x + 64 + col, f.slots);
+        }
+        if (ok == 0) continue;
+        uint32_t quad[4];
+        if (DROP) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t lo = __builtin_amdgcn_readlane(word, 8 * u), hi = __builtin_amdgcn_readlane(word, 8 * u + 4);
+                quad[u] = h ? hi : lo;
+            }
+        }
+        Weights<T> w[NA];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            f16v s = dot<D>(k, q[n], f16v{});
+            f16v p = dot<D>(v, g[n], f16v{});           // dP
+            if (ok != 0xffffffffu) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!((ok >> acc_row(r, 0)) >> (4 * h) & 1)) s[r] = -INFINITY;
+            }
+            if (DROP) {
+                uint32_t words[4][2];
+                row_keep(a.rnd, call, quad, (uint32_t)i * a.pairs + ((row0 + 32 * n + col) >> 1), bm, words);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    p[r] = (words[r >> 2][(r & 3) >> 1] >> (16 * (r & 1)) & 0xffffu) < a.rnd.threshold ? 0.0f : p[r] * keep;
+            }
+            f16v ds;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -row_lse[n]));
+                if (FIX) D1[n] = __builtin_fmaf(s[r], p[r], D1[n]);
+                ds[r] = s[r] * (p[r] - D0[n]);
+            }
+            w[n].set(ds);
+            if (FIX) w[NR + n].set(s);
+        }
+        accumulate<D, NA>(acc, tile, w, lane);
+    }
+
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        const float exact = FIX ? halves_sum(D1[n]) : D0[n], fix = FIX ? exact - D0[n] : 0.0f;
+        const int r = row0 + 32 * n + col;
+        if (h == 0 && r < f.row_tiles * 32) {
+            const long long at = (long long)group * f.row_tiles * 32 + r;
+            f.row_lse[at] = row_lse[n];
+            f.row_D[at] = exact;
+        }
+        if (out_at[n] < 0) continue;
+        const bool valid = row_lse[n] != INFINITY;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int u = 0; u < 16; u += 4) {
+                const int c = 32 * dt + acc_row(u, h);
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = acc[n][dt][u + e];
+                    if (FIX) x[e] = __builtin_fmaf(-fix, acc[NA - NR + n][dt][u + e], x[e]);
+                    x[e] = valid ? x[e] * a.scale : 0.0f;
+                }
+                store4((T*)f.dq + out_at[n] + c, x, a.d - c, f.vec_dq);
+            }
+    }
+}
+
+// The lists turned around: one wave per region of keys goes over all entries of its image and head.
+__global__ __launch_bounds__(256) void region_invert_kernel(BwdArgs f)
+{
+    const Args& a = f.a;
+    const int lane = threadIdx.x & 63;
+    const long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int J = a.km.regions;
+    if (id >= (long long)a.B * a.kv * J) return;
+    const int bm = (int)(id / J), j = (int)(id - (long long)bm * J);
+    const int* list = a.index + (long long)bm * f.entries;
+    int less = 0, mine = 0;
+    for (int e = lane; e < f.entries; e += 64) {
+        const int x = list[e];
+        less += x >= 0 && x < j;
+        mine += x == j;
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) { less += __shfl_xor(less, s); mine += __shfl_xor(mine, s); }
+    if (lane == 0) {
+        f.start[(long long)bm * (J + 1) + j] = less;
+        if (j == J - 1) f.start[(long long)bm * (J + 1) + J] = less + mine;
+    }
+    if (mine == 0) return;
+    int2* to = f.sorted + (long long)bm * f.entries + less;
+    for (int e0 = 0; e0 < f.entries; e0 += 64) {
+        const int e = e0 + lane;
+        const bool hit = e < f.entries && list[e] == j;
+        const uint64_t mask = __ballot(hit);
+        if (hit) to[__popcll(mask & ((1ull << lane) - 1))] = int2{e / a.T, j};
+        to += __popcll(mask);
+    }
+}
+
+// Random bits seen from a key (lane) and 16 rows (registers): a patch of 4 keys and 2 rows is four lanes wide, so each of four lanes makes two
+// of their eight evaluations.  Returns for row pair p (registers 2 p, 2 p + 1) the two words that hold this lane's keys.
+__device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint32_t quad, uint32_t pair0, int h, uint32_t bm, uint32_t (&words)[8][2])
+{
+    const int k = threadIdx.x & 3;
+    Words x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int p = 4 * u + k;                // rows acc_row(2 p, h) and the next
+        x[u] = philox(quad, pair0 + 4 * (p >> 1) + 2 * h + (p & 1), bm, call, rnd.key0, rnd.key1);
+    }
+    auto from = [&](auto lane4, uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp(v, decltype(lane4)::value * 0x55, 0xf, 0xf, true); };
+    auto pairs = [&](auto lane4) {
+        constexpr int p = decltype(lane4)::value;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t lo = from(lane4, x[u].w[2 * e]), hi = from(lane4, x[u].w[2 * e + 1]);
+                words[4 * u + p][e] = k & 2 ? hi : lo;
+            }
+    };
+    pairs(std::integral_constant<int, 0>{}); pairs(std::integral_constant<int, 1>{});
+    pairs(std::integral_constant<int, 2>{}); pairs(std::integral_constant<int, 3>{});
+}
+
+// dk and dv of 32 NK keys of a region.
+template <typename T, int D, int NK, bool DROP>
+__global__ __launch_bounds__(256) void region_dkdv_kernel(BwdArgs f)
+{
+    const Args& a = f.a;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int item = (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
+    if (item >= f.items) return;
+    constexpr int ROOM = 2 * Tile<T, D>::BYTES + 256;
+    unsigned char* tile_q = lds + wave * ROOM;
+    unsigned char* tile_g = tile_q + Tile<T, D>::BYTES;
+    float* stat = (float*)(tile_g + Tile<T, D>::BYTES);        // lse, then D, of 32 rows
+    const int J = a.km.regions, col = lane & 31, h = lane >> 5;
+
+    // this wave's work: the first `share` entries of a region (units 0 .. J - 1), or those of a window that lie beyond (the rest)
+    const int per_image = (J + f.windows) * f.key_tiles;
+    const int bm = item / per_image;
+    int unit = item - bm * per_image;
+    const int kt = unit % f.key_tiles;
+    unit /= f.key_tiles;
+    const int b = bm / a.kv, m = bm - b * a.kv;
+    const int* start = f.start + (long long)bm * (J + 1);
+    const int2* sorted = f.sorted + (long long)bm * f.entries;
+    int j = unit, from, to, slot = -1;
+    if (unit < J) {
+        from = start[j];
+        const int end = start[j + 1];
+        to = min(end, from + f.share);
+        if (end > to) slot = 2 * (from / f.share);
+    } else {
+        const int window = unit - J;
+        if ((long long)window * f.share >= start[J]) return;
+        j = sorted[window * f.share].y;
+        from = max(window * f.share, start[j] + f.share);
+        to = min(start[j + 1], (window + 1) * f.share);
+        if (from >= to) return;
+        slot = 2 * window + 1;
+    }
+    j = __builtin_amdgcn_readfirstlane(j); from = __builtin_amdgcn_readfirstlane(from); to = __builtin_amdgcn_readfirstlane(to);
+    slot = __builtin_amdgcn_readfirstlane(slot);
+
+    Operand<T, D> k[NK], v[NK];
+    long long out_at[NK];
+    bool valid[NK];
+    uint32_t quad[NK];
+    {
+        int vh, vw;
+        a.km.limits(b, vh, vw);
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            const int place = (kt * NK + n) * 32 + col;
+            const int px = place < a.km.places ? a.km.pixel(j, place, a.km.H, a.km.W) : -1;
+            valid[n] = place < a.km.places && a.km.pixel(j, place, vh, vw) >= 0;
+            const long long n_px = (long long)a.km.H * a.km.W;
+            out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.kv * a.d + m * a.d;
+            quad[n] = (uint32_t)j * a.quads + (place >> 2);
+            const long long at = valid[n] ? px : 0;
+            load_operand<T, D>(k[n], (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.d, valid[n], a.d, h, f.vec_k);
+            load_operand<T, D>(v[n], (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.d, valid[n], a.d, h, f.vec_v);
+        }
+    }
+    const uint32_t call = DROP ? a.rnd.call() : 0;
+    const float c2 = a.scale * LOG2E, keep = DROP ? a.rnd.scale : 1.0f;
+    f16v dk[NK][D / 32], dv[NK][D / 32];
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) { dk[n][dt] = f16v{}; dv[n][dt] = f16v{}; }
+
+    int qh, qw;
+    a.qm.limits(b, qh, qw);
+    const long long n_px = (long long)a.qm.H * a.qm.W;
+    Operand<T, D> q, g;
+    float st;
+    // step s: row tile s % row_tiles of the group of entry from + s / row_tiles
+    const int steps = (to - from) * f.row_tiles;
+    auto group_of = [&](int s) { return s < steps ? sorted[from + f.by_row_tiles.of(s)].x : 0; };
+    auto fetch = [&](int s, int i) {
+        const int r = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32 + col;
+        const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
+        const int px = r < a.R ? a.qm.pixel(i, place, qh, qw) : -1;
+        const bool ok = px >= 0;
+        load_operand<T, D>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h, f.vec_q);
+        load_operand<T, D>(g, (const T*)f.dout + (ok ? ((long long)b * n_px + px) * a.heads * a.d + head * a.d : 0), ok, a.d, h, f.vec_do);
+        st = (h ? f.row_D : f.row_lse)[((long long)bm * a.qm.regions + i) * f.row_tiles * 32 + r];
+    };
+    int next = group_of(0), i = next;
+    if (steps > 0) fetch(0, next);
+    next = group_of(1);
+    for (int s = 0; s < steps; ++s) {
+        const int r0 = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32;
+        wave_order();
+        stage<D>(tile_q, q, lane);
+        stage<D>(tile_g, g, lane);
+        stat[lane] = st;
+        wave_order();
+        const Operand<T, D> qc = q, gc = g;
+        const uint32_t pair0 = (uint32_t)i * a.pairs + (r0 >> 1);
+        if (s + 1 < steps) {
+            fetch(s + 1, next);
+            i = next;
+            next = group_of(s + 2);
+        }
+        float lse[16], Dr[16];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f4 x = *(const f4*)(stat + acc_row(4 * u, h)), y = *(const f4*)(stat + 32 + acc_row(4 * u, h));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { lse[4 * u + e] = x[e]; Dr[4 * u + e] = y[e]; }
+        }
+        Weights<T> wk[NK], wv[NK];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+            f16v p = dot<D>(qc, k[n], f16v{});
+            f16v ds = dot<D>(gc, v[n], f16v{});
+            uint32_t words[8][2];
+            if (DROP) key_keep(a.rnd, call, quad[n], pair0, h, bm, words);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c2, -lse[r]));
+                bool kept = true;
+                if (DROP) kept = (words[r >> 1][r & 1] >> (16 * (lane & 1)) & 0xffffu) >= a.rnd.threshold;
+                ds[r] = p[r] * ((kept ? (DROP ? ds[r] * keep : ds[r]) : 0.0f) - Dr[r]);
+                if (DROP && !kept) p[r] = 0.0f;
+            }
+            wv[n].set(p);
+            wk[n].set(ds);
+        }
+        accumulate<D, NK>(dv, tile_g, wv, lane);
+        accumulate<D, NK>(dk, tile_q, wk, lane);
+    }
+
+    float* part = f.partial + (((long long)bm * f.key_tiles + kt) * 2 * f.windows + max(slot, 0)) * (2 * 32 * NK * D);
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int u = 0; u < 16; u += 4) {
+                const int c = 32 * dt + acc_row(u, h);
+                float x[4], y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = valid[n] ? dk[n][dt][u + e] * a.scale : 0.0f;
+                    y[e] = valid[n] ? dv[n][dt][u + e] * keep : 0.0f;
+                }
+                if (slot >= 0) {
+                    float* p = part + (32 * n + col) * D + c;
+                    *(f4*)p = f4{x[0], x[1], x[2], x[3]};
+                    *(f4*)(p + 32 * NK * D) = f4{y[0], y[1], y[2], y[3]};
+                } else if (out_at[n] >= 0) {
+                    store4((T*)f.dk + out_at[n] + c, x, a.d - c, f.vec_dk);
+                    store4((T*)f.dv + out_at[n] + c, y, a.d - c, f.vec_dk);
+                }
+            }
+}
+
+// The regions that more than `share` groups list: adds up the float32 sums of their waves, in order.
+template <typename T, int D, int NK>
+__global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
+{
+    const Args& a = f.a;
+    const int J = a.km.regions;
+    const int window = blockIdx.x % f.windows, kt = blockIdx.x / f.windows % f.key_tiles, bm = blockIdx.x / f.windows / f.key_tiles;
+    const int b = bm / a.kv, m = bm - b * a.kv;
+    const int* start = f.start + (long long)bm * (J + 1);
+    // a region whose first wave wrote to this window reaches into the next one
+    if ((long long)(window + 1) * f.share >= start[J]) return;
+    const int j = f.sorted[(long long)bm * f.entries + (window + 1) * f.share].y;
+    const int s = start[j], e = start[j + 1];
+    if (s / f.share != window || e - s <= f.share) return;
+    const float* part = f.partial + ((long long)bm * f.key_tiles + kt) * 2 * f.windows * (2 * 32 * NK * D);
+    const int last = (e - 1) / f.share;
+    for (int u = threadIdx.x; u < 2 * 32 * NK * D / 4; u += 256) {
+        f4 sum = *(const f4*)(part + (long long)(2 * window) * (2 * 32 * NK * D) + 4 * u);
+        for (int w = (s + f.share) / f.share; w <= last; ++w) sum += *(const f4*)(part + (long long)(2 * w + 1) * (2 * 32 * NK * D) + 4 * u);
+        const int c = 4 * u % D, place = kt * 32 * NK + 4 * u / D % (32 * NK), side = 4 * u / D / (32 * NK);
+        const int px = place < a.km.places ? a.km.pixel(j, place, a.km.H, a.km.W) : -1;
+        if (px < 0) continue;
+        const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
+        store4((T*)(side ? f.dv : f.dk) + ((long long)b * a.km.H * a.km.W + px) * a.kv * a.d + m * a.d + c, x, a.d - c, f.vec_dk);
+    }
+}
+
+// Two row tiles (or tiles of keys) per wave halve the reads of the other side's operands, where the registers hold them: the
+// sums take 2 x 16 registers per tile and 32 channels.
+template <typename T> static bool two_tiles(const Args& a, int n) { return sizeof(T) == 2 && a.d <= 32 && n > 32; }
+
+static int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+// sizes that the workspace and the launches share
+template <typename T> static void plan(BwdArgs& f)
+{
+    const Args& a = f.a;
+    f.slots = 4 * a.quads * a.T;
+    f.row_tiles = (a.R + 31) / 32;
+    f.by_row_tiles = Div::by(f.row_tiles);
+    f.key_tiles = (a.km.places + (two_tiles<T>(a, a.km.places) ? 63 : 31)) / (two_tiles<T>(a, a.km.places) ? 64 : 32);
+    f.entries = a.qm.regions * a.T;
+    // A wave's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip
+    const long long average = ((long long)f.entries + a.km.regions - 1) / a.km.regions;
+    const long long all = (long long)a.B * a.kv * f.key_tiles * f.entries;
+    const long long fill = std::max(1ll, all / (8ll * device_cu_count()));
+    f.share = (int)std::min(std::max(2 * average, (8ll + f.row_tiles - 1) / f.row_tiles), fill);
+    f.windows = (f.entries + f.share - 1) / f.share;
+}
+
+struct Room { size_t lse, D, sorted, start, partial, end; };
+
+template <typename T> static Room room(const BwdArgs& f)
+{
+    const Args& a = f.a;
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    const size_t bm = (size_t)a.B * a.kv, rows = bm * a.qm.regions * f.row_tiles * 32 * sizeof(float);
+    const int nk = two_tiles<T>(a, a.km.places) ? 2 : 1;
+    Room r;
+    r.lse = 0;
+    r.D = up(rows);
+    r.sorted = r.D + up(rows);
+    r.start = r.sorted + up(bm * f.entries * sizeof(int2));
+    r.partial = r.start + up(bm * (a.km.regions + 1) * sizeof(int));
+    r.end = r.partial + bm * f.key_tiles * 2 * f.windows * (2 * 32 * nk * padded(a.d)) * sizeof(float);
+    return r;
+}
+
+template <typename T> static size_t bytes_t(const Args& a)
+{
+    BwdArgs f{};
+    f.a = a;
+    plan<T>(f);
+    return room<T>(f).end;
+}
+
+size_t bwd_workspace_bytes(const Args& a) { return a.dtype == 0 ? bytes_t<float>(a) : bytes_t<bf16_bits>(a); }
+
+template <typename T, int D, int NR>
+static hipError_t run_rows(BwdArgs& f, hipStream_t st)
+{
+    f.tiles = (f.a.R + 32 * NR - 1) / (32 * NR);
+    f.items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
+    const int blocks = (f.items + 3) / 4, lds = 4 * Tile<T, D>::BYTES;
+    if (f.a.rnd.threshold) region_dq_kernel<T, D, NR, true><<<blocks, 256, lds, st>>>(f);
+    else region_dq_kernel<T, D, NR, false><<<blocks, 256, lds, st>>>(f);
+    return hipGetLastError();
+}
+
+template <typename T, int D, int NK>
+static hipError_t run_keys(BwdArgs& f, hipStream_t st)
+{
+    const long long items = (long long)f.a.B * f.a.kv * f.key_tiles * (f.a.km.regions + f.windows);
+    f.items = (int)items;
+    const int blocks = (f.items + 3) / 4, lds = 4 * (2 * Tile<T, D>::BYTES + 256);
+    static LdsOptIn opt;
+    hipError_t e = opt.ensure({(const void*)region_dkdv_kernel<T, D, NK, true>, (const void*)region_dkdv_kernel<T, D, NK, false>}, lds);
+    if (e != hipSuccess) return e;
+    if (f.a.rnd.threshold) region_dkdv_kernel<T, D, NK, true><<<blocks, 256, lds, st>>>(f);
+    else region_dkdv_kernel<T, D, NK, false><<<blocks, 256, lds, st>>>(f);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (f.entries > f.share) {
+        region_dkdv_join_kernel<T, D, NK><<<f.a.B * f.a.kv * f.key_tiles * f.windows, 256, 0, st>>>(f);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <typename T>
+static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
+{
+    const Args& a = f.a;
+    plan<T>(f);
+    const Room r = room<T>(f);
+    f.row_lse = (float*)(ws + r.lse); f.row_D = (float*)(ws + r.D); f.sorted = (int2*)(ws + r.sorted);
+    f.start = (int*)(ws + r.start); f.partial = (float*)(ws + r.partial);
+    const Strides whole{(long long)a.heads * a.d, (long long)a.qm.H * a.qm.W * a.heads * a.d};
+    f.vec_q = pieces(a.q, a.qs, a.d, sizeof(T));
+    f.vec_k = pieces(a.k, a.ks, a.d, sizeof(T));
+    f.vec_v = pieces(a.v, a.vs, a.d, sizeof(T));
+    f.vec_do = pieces(f.dout, whole, a.d, sizeof(T));
+    f.vec_o = pieces(f.out, whole, a.d, sizeof(T));
+    const uintptr_t quad = 4 * sizeof(T) - 1;
+    f.vec_dq = a.d % 4 == 0 && ((uintptr_t)f.dq & quad) == 0;
+    f.vec_dk = a.d % 4 == 0 && ((uintptr_t)f.dk & quad) == 0 && ((uintptr_t)f.dv & quad) == 0;
+    hipError_t e;
+    if (two_tiles<T>(a, a.R)) e = run_rows<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
+    else e = a.d <= 32 ? run_rows<T, 32, 1>(f, st) : a.d <= 64 ? run_rows<T, 64, 1>(f, st) : run_rows<T, 128, 1>(f, st);
+    if (e != hipSuccess) return e;
+    region_invert_kernel<<<(int)(((long long)a.B * a.kv * a.km.regions + 3) / 4), 256, 0, st>>>(f);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (two_tiles<T>(a, a.km.places)) return run_keys<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
+    return a.d <= 32 ? run_keys<T, 32, 1>(f, st) : a.d <= 64 ? run_keys<T, 64, 1>(f, st) : run_keys<T, 128, 1>(f, st);
+}
+
+hipError_t launch_bwd(const Args& a, const void* dout, const void* out, const float* lse, void* dq, void* dk, void* dv,
+                      void* workspace, hipStream_t st)
+{
+    BwdArgs f{};
+    f.a = a; f.dout = dout; f.out = out; f.lse = lse; f.dq = dq; f.dk = dk; f.dv = dv;
+    return a.dtype == 0 ? run_t<float>(f, (unsigned char*)workspace, st) : run_t<bf16_bits>(f, (unsigned char*)workspace, st);
+}
+
+}  // namespace region
+}  // namespace slide

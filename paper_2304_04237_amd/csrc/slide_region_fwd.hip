@@ -20,43 +20,6 @@ struct FwdArgs {
     int items;              // waves with work
 };
 
-// The keys of a group: slot x of the concatenated regions -> pixel.
-struct Walk {
-    const int* list;
-    int vh, vw;             // valid height and width of the image
-    int entry, place;       // of this lane's slot in the tile that is looked up next
-    __device__ __forceinline__ int look(const Args& a, int x, int end)
-    {
-        entry = a.by_slots.of(x);
-        place = x - entry * 4 * a.quads;
-        return x < end ? list[entry] : -1;
-    }
-    // pixel of (region j, place), -1 if there is none
-    static __device__ __forceinline__ int pixel(const Args& a, int j, int place, int vh, int vw)
-    {
-        return j >= 0 && j < a.km.regions && place < a.km.places ? a.km.pixel(j, place, vh, vw) : -1;
-    }
-};
-
-// Random bits of the attention weights of one row tile: this lane's row (its pair and parity) and its 16 keys, quad q of which has
-// counter word quad[q].  Two rows share an evaluation, so each lane of a pair makes half of them and passes on what the other needs.
-__device__ __forceinline__ void row_keep(const Random& rnd, uint32_t call, const uint32_t (&quad)[4], uint32_t pair, uint32_t bm, uint32_t (&words)[4][2])
-{
-    const bool odd = threadIdx.x & 1;
-    Words x[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) x[u] = philox(odd ? quad[2 + u] : quad[u], pair, bm, call, rnd.key0, rnd.key1);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t mine = odd ? x[u].w[2 + e] : x[u].w[e], pass = odd ? x[u].w[e] : x[u].w[2 + e];
-            const uint32_t got = __builtin_amdgcn_mov_dpp(pass, 0xB1, 0xf, 0xf, true);         // from lane ^ 1
-            words[u][e] = odd ? got : mine;
-            words[2 + u][e] = odd ? mine : got;
-        }
-}
-
 template <typename T, int D, int NR, bool DROP>
 __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
 {
@@ -199,12 +162,6 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
             }
         if (h == 0 && f.lse) f.lse[lse_at[n] >> 1] = !valid || total == 0.0f ? -INFINITY : (sub[n] + log2f(total)) * LN2;
     }
-}
-
-static bool pieces(const void* p, const Strides& s, int d, size_t esz)
-{
-    const long long n = 16 / esz;
-    return ((uintptr_t)p & 15) == 0 && s.pixel % n == 0 && s.image % n == 0 && d % n == 0;
 }
 
 template <typename T, int D, int NR>
