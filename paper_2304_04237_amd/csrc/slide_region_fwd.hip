@@ -5,6 +5,10 @@
 // between the lane halves), P = exp2(S c - m) with a running maximum m and sum, O^T += V^T P^T.  P stays in the registers in which the
 // first product leaves it.  K goes from memory into operands, V through 32 rows of LDS that only this wave uses; both are loaded
 // one tile ahead.  Waves share nothing, so no barrier is passed and the waves of a compute unit cover each other's latencies.
+//
+// Few rows over many keys (one new token) leave most of the chip idle that way.  Then the keys of a group are split: the four waves
+// of a block take a quarter each of a share of the keys and join their sums in LDS, and where one block per 32 rows is still too
+// little, shares go to several blocks, whose float32 sums a second kernel joins.
 #include "slide_region_mma.h"
 
 namespace slide {
@@ -17,18 +21,35 @@ struct FwdArgs {
     int tiles;              // of 32 NR rows in a group
     int slots;              // keys of a group, with every listed region's slots a multiple of 4
     int vec_q, vec_k, vec_v, vec_o;
-    int items;              // waves with work
+    int items;              // waves (SPLIT: blocks) with work
+    int shares;             // SPLIT: blocks that share the keys of 32 rows
+    float* part;            // SPLIT, shares > 1: [rows' item][share][32][D] sums, then [2][32] maxima and sums
 };
 
-template <typename T, int D, int NR, bool DROP>
+// out and lse of a row from its sums: o[0..3] channels c ..
+template <typename T>
+__device__ __forceinline__ void finish(const FwdArgs& f, long long out_at, int c, const float (&o)[4], float up)
+{
+    const float x[4] = {up != 0.0f ? o[0] * up : 0.0f, up != 0.0f ? o[1] * up : 0.0f, up != 0.0f ? o[2] * up : 0.0f, up != 0.0f ? o[3] * up : 0.0f};
+    store4((T*)f.out + out_at + c, x, f.a.d - c, f.vec_o);
+}
+
+template <typename T, int D, int NR, bool DROP, bool SPLIT>
 __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
 {
     const Args& a = f.a;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int item = (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
-    if (item >= f.items) return;
+    const int work = SPLIT ? (int)xcd_order(blockIdx.x, gridDim.x) : (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
+    if (work >= f.items) return;
+    const int item = SPLIT ? work / f.shares : work, share = SPLIT ? work - item * f.shares : 0;
     unsigned char* tile = lds + wave * Tile<T, D>::BYTES;
+    int first = 0, end = f.slots;
+    if (SPLIT) {
+        const int key_tiles = (f.slots + 31) / 32, parts = 4 * f.shares, w = 4 * share + wave;
+        first = (int)((long long)key_tiles * w / parts) * 32;
+        end = min(f.slots, (int)((long long)key_tiles * (w + 1) / parts) * 32);
+    }
     const int group = item / f.tiles, row0 = (item - group * f.tiles) * 32 * NR;
     const int bm = group / a.qm.regions, i = group - bm * a.qm.regions;
     const int b = bm / a.kv, m = bm - b * a.kv;
@@ -70,7 +91,7 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
     Operand<T, D> k[2], v;
-    int region = walk.look(a, col, f.slots);
+    int region = walk.look(a, first + col, end);
     uint32_t word, next_word = 0;
     uint32_t ok, next_ok;
     auto fetch = [&](Operand<T, D>& kk) {
@@ -80,17 +101,19 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         load_operand<T, D>(kk, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h, f.vec_k);
         load_operand<T, D>(v, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h, f.vec_v);
     };
-    fetch(k[0]);
-    region = walk.look(a, 32 + col, f.slots);
+    if (first < end) {
+        fetch(k[0]);
+        region = walk.look(a, first + 32 + col, end);
+    }
 
     auto step = [&](const Operand<T, D>& kk, Operand<T, D>& kn, int x) {
         ok = next_ok; word = next_word;
         wave_order();
         stage<D>(tile, v, lane);
         wave_order();
-        if (x + 32 < f.slots) {
+        if (x + 32 < end) {
             fetch(kn);
-            region = walk.look(a, x + 64 + col, f.slots);
+            region = walk.look(a, x + 64 + col, end);
         }
         if (ok == 0) return;
         uint32_t quad[4];
@@ -140,28 +163,161 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         }
         accumulate<D, NR>(o, tile, w, lane);
     };
-    for (int x = 0; x < f.slots; x += 64) {
+    for (int x = first; x < end; x += 64) {
         step(k[0], k[1], x);
-        if (x + 32 < f.slots) step(k[1], k[0], x + 32);
+        if (x + 32 < end) step(k[1], k[0], x + 32);
     }
 
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        const float total = halves_sum(sum[n]);
-        if (out_at[n] < 0) continue;
-        const bool valid = lse_at[n] & 1;
-        const float up = !valid || total == 0.0f ? 0.0f : (DROP ? a.rnd.scale : 1.0f) / total;
+    if constexpr (SPLIT) {
+        // [wave][D][32] sums and [wave][2][32] maxima and sums; thread: row col, every eighth quad of channels
+        static_assert(NR == 1, "the split form takes 32 rows");
+        float* sums = (float*)lds;
+        float* stat = sums + 4 * D * 32;
+        const float total = halves_sum(sum[0]);
+        __syncthreads();                                    // (the tiles are in the same place)
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int c = 32 * dt + acc_row(r, h);
-                const float x[4] = {valid ? o[n][dt][r] * up : 0.0f, valid ? o[n][dt][r + 1] * up : 0.0f,
-                                    valid ? o[n][dt][r + 2] * up : 0.0f, valid ? o[n][dt][r + 3] * up : 0.0f};
-                store4((T*)f.out + out_at[n] + c, x, a.d - c, f.vec_o);
+            for (int r = 0; r < 16; ++r) sums[(wave * D + 32 * dt + acc_row(r, h)) * 32 + col] = o[0][dt][r];
+        if (h == 0) { stat[wave * 64 + col] = top[0]; stat[wave * 64 + 32 + col] = total; }
+        __syncthreads();
+        float most = -INFINITY, all = 0.0f, back[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, stat[w * 64 + col]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float t = stat[w * 64 + col];
+            back[w] = t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - most);
+            all += back[w] * stat[w * 64 + 32 + col];
+        }
+        if (out_at[0] < 0) return;
+        const bool valid = lse_at[0] & 1;
+        float* part = f.part + ((long long)item * f.shares + share) * (D * 32 + 64);
+        const float up = !valid || all == 0.0f ? 0.0f : (DROP ? a.rnd.scale : 1.0f) / all;
+        for (int c = 4 * (threadIdx.x >> 5); c < D; c += 32) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x[e] = __builtin_fmaf(back[w], sums[(w * D + c + e) * 32 + col], x[e]);
             }
-        if (h == 0 && f.lse) f.lse[lse_at[n] >> 1] = !valid || total == 0.0f ? -INFINITY : (sub[n] + log2f(total)) * LN2;
+            if (f.shares == 1) {
+                finish<T>(f, out_at[0], c, x, up);
+            } else {
+                *(f4*)(part + col * D + c) = f4{x[0], x[1], x[2], x[3]};
+            }
+        }
+        if (threadIdx.x < 32) {
+            if (f.shares > 1) { part[D * 32 + col] = most; part[D * 32 + 32 + col] = all; }
+            else if (f.lse) f.lse[lse_at[0] >> 1] = up == 0.0f ? -INFINITY : ((most == -INFINITY ? 0.0f : most) + log2f(all)) * LN2;
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const float total = halves_sum(sum[n]);
+            if (out_at[n] < 0) continue;
+            const float up = !(lse_at[n] & 1) || total == 0.0f ? 0.0f : (DROP ? a.rnd.scale : 1.0f) / total;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const float x[4] = {o[n][dt][r], o[n][dt][r + 1], o[n][dt][r + 2], o[n][dt][r + 3]};
+                    finish<T>(f, out_at[n], 32 * dt + acc_row(r, h), x, up);
+                }
+            if (h == 0 && f.lse) f.lse[lse_at[n] >> 1] = up == 0.0f ? -INFINITY : (sub[n] + log2f(total)) * LN2;
+        }
     }
+}
+
+// Joins the sums of the blocks that shared a row's keys.  One wave per row of 32; a lane takes D / 64 channels.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void region_fwd_join_kernel(FwdArgs f)
+{
+    const Args& a = f.a;
+    const int lane = threadIdx.x & 63, item = blockIdx.x, group = item / f.tiles;
+    const int col = 4 * blockIdx.y + (threadIdx.x >> 6), r = (item - group * f.tiles) * 32 + col;
+    if (r >= a.R) return;
+    const int bm = group / a.qm.regions, i = group - bm * a.qm.regions, b = bm / a.kv, m = bm - b * a.kv;
+    const int place = a.by_g.of(r), head = m * a.g + r - place * a.g, px = a.qm.pixel(i, place, a.qm.H, a.qm.W);
+    if (px < 0) return;
+    int vh, vw;
+    a.qm.limits(b, vh, vw);
+    const bool valid = a.qm.pixel(i, place, vh, vw) >= 0;
+    constexpr int SIZE = D * 32 + 64;
+    const float* part = f.part + (long long)item * f.shares * SIZE;
+    float most = -INFINITY, all = 0.0f, x[(D + 63) / 64] = {};
+    for (int s = lane; s < f.shares; s += 64) most = fmaxf(most, part[(long long)s * SIZE + D * 32 + col]);
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) most = fmaxf(most, __shfl_xor(most, w));
+    for (int s0 = 0; s0 < f.shares; s0 += 64) {
+        const int s = s0 + lane;
+        const float* p = part + (long long)s * SIZE + D * 32 + col;
+        const float t = s < f.shares ? p[0] : -INFINITY;
+        const float mine = t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - most);
+        float sum = s < f.shares ? mine * p[32] : 0.0f;
+#pragma unroll
+        for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
+        all += sum;
+        const int n = min(64, f.shares - s0);
+#pragma unroll 8
+        for (int k = 0; k < n; ++k) {
+            const float back = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), k));
+            const float* from = part + (long long)(s0 + k) * SIZE + col * D;
+#pragma unroll
+            for (int u = 0; u < (D + 63) / 64; ++u)
+                if (lane + 64 * u < D) x[u] = __builtin_fmaf(back, from[lane + 64 * u], x[u]);
+        }
+    }
+    const float up = !valid || all == 0.0f ? 0.0f : a.rnd.scale / all;
+    const long long n_px = (long long)a.qm.H * a.qm.W, at = ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
+#pragma unroll
+    for (int u = 0; u < (D + 63) / 64; ++u)
+        if (lane + 64 * u < a.d) Elem<T>::store((T*)f.out + at + lane + 64 * u, up != 0.0f ? x[u] * up : 0.0f);
+    if (lane == 0 && f.lse)
+        f.lse[((long long)b * a.heads + head) * n_px + px] = up == 0.0f ? -INFINITY : ((most == -INFINITY ? 0.0f : most) + log2f(all)) * LN2;
+}
+
+// How a problem is cut.  A block per 32 rows and share of the keys (SPLIT) where a wave per 32 rows would not give every SIMD one;
+// then as many shares as give every SIMD one, of at least two key tiles each.
+struct Cut { bool split; int tiles, shares; };
+
+static Cut cut(const Args& a)
+{
+    const int cus = device_cu_count();
+    const long long groups = (long long)a.B * a.kv * a.qm.regions;
+    Cut c{false, (a.R + 31) / 32, 1};
+    const long long items = groups * c.tiles;
+    const int key_tiles = (4 * a.quads * a.T + 31) / 32;
+    c.split = items < 4ll * cus && key_tiles > 1;
+    if (c.split) c.shares = (int)std::max(1ll, std::min((cus + items - 1) / items, (long long)key_tiles / 8));
+    return c;
+}
+
+static int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+size_t fwd_workspace_bytes(const Args& a)
+{
+    const Cut c = cut(a);
+    return c.shares > 1 ? (size_t)a.B * a.kv * a.qm.regions * c.tiles * c.shares * (padded(a.d) * 32 + 64) * sizeof(float) : 0;
+}
+
+template <typename T, int D>
+static hipError_t run_split(FwdArgs& f, const Cut& c, hipStream_t st)
+{
+    f.tiles = c.tiles;
+    f.shares = c.shares;
+    const int items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
+    f.items = items * f.shares;
+    const int lds = std::max(4 * Tile<T, D>::BYTES, 4 * (D * 32 + 64) * (int)sizeof(float));
+    static LdsOptIn opt;
+    hipError_t e = opt.ensure({(const void*)region_fwd_kernel<T, D, 1, true, true>, (const void*)region_fwd_kernel<T, D, 1, false, true>}, lds);
+    if (e != hipSuccess) return e;
+    if (f.a.rnd.threshold) region_fwd_kernel<T, D, 1, true, true><<<f.items, 256, lds, st>>>(f);
+    else region_fwd_kernel<T, D, 1, false, true><<<f.items, 256, lds, st>>>(f);
+    if ((e = hipGetLastError()) != hipSuccess || f.shares == 1) return e;
+    region_fwd_join_kernel<T, D><<<dim3(items, (std::min(f.a.R, 32) + 3) / 4), 256, 0, st>>>(f);
+    return hipGetLastError();
 }
 
 template <typename T, int D, int NR>
@@ -171,8 +327,8 @@ static hipError_t run(FwdArgs& f, hipStream_t st)
     const long long items = (long long)f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
     f.items = (int)items;
     const int blocks = (int)((items + 3) / 4), lds = 4 * Tile<T, D>::BYTES;
-    if (f.a.rnd.threshold) region_fwd_kernel<T, D, NR, true><<<blocks, 256, lds, st>>>(f);
-    else region_fwd_kernel<T, D, NR, false><<<blocks, 256, lds, st>>>(f);
+    if (f.a.rnd.threshold) region_fwd_kernel<T, D, NR, true, false><<<blocks, 256, lds, st>>>(f);
+    else region_fwd_kernel<T, D, NR, false, false><<<blocks, 256, lds, st>>>(f);
     return hipGetLastError();
 }
 
@@ -184,6 +340,8 @@ static hipError_t run_t(FwdArgs& f, hipStream_t st)
     f.vec_k = pieces(a.k, a.ks, a.d, sizeof(T));
     f.vec_v = pieces(a.v, a.vs, a.d, sizeof(T));
     f.vec_o = a.d % 4 == 0 && ((uintptr_t)f.out & (4 * sizeof(T) - 1)) == 0;
+    const Cut c = cut(a);
+    if (c.split) return a.d <= 32 ? run_split<T, 32>(f, c, st) : a.d <= 64 ? run_split<T, 64>(f, c, st) : run_split<T, 128>(f, c, st);
     // two row tiles per wave read every key operand half as often, where the registers hold them
     const bool two = a.R > 32;
     if (a.d <= 32) return two ? run<T, 32, 2>(f, st) : run<T, 32, 1>(f, st);
@@ -191,12 +349,10 @@ static hipError_t run_t(FwdArgs& f, hipStream_t st)
     return run<T, 128, 1>(f, st);
 }
 
-size_t fwd_workspace_bytes(const Args&) { return 0; }
-
-hipError_t launch_fwd(const Args& a, void* out, float* lse, void*, hipStream_t st)
+hipError_t launch_fwd(const Args& a, void* out, float* lse, void* workspace, hipStream_t st)
 {
     FwdArgs f{};
-    f.a = a; f.out = out; f.lse = lse;
+    f.a = a; f.out = out; f.lse = lse; f.part = (float*)workspace;
     f.slots = 4 * a.quads * a.T;
     return a.dtype == 0 ? run_t<float>(f, st) : run_t<bf16_bits>(f, st);
 }

@@ -14,7 +14,7 @@ typedef double d4 __attribute__((ext_vector_type(4)));
 typedef double d2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr int POOL = 256;               // threads of a pooling block
+constexpr int POOL = 256, PICK = 512;       // threads of a pooling and of a picking block
 
 // One side of the problem (queries, or keys with g = 1) as the pooling kernel sees it.  A thread owns one piece (E channels) of one
 // key head and every lanes-th place of its region; a block takes `packed` regions if they are small, and `together` key heads.
@@ -180,24 +180,24 @@ __device__ __forceinline__ void pick(Get get, int chunks, int T, int* list)
 }
 
 // NG groups of one key head per block: scores of 16 x 16 groups and regions by v_mfma_f64_16x16x4_f64 (left lane: group lane % 16, channels
-// (lane / 16) dp / 4 ..; right likewise the region; register r of the result: group 4 r + lane / 16, region lane % 16), then one
+// 8 s + 2 (lane / 16) and the next; right likewise the region; register r of the result: group 4 r + lane / 16, region lane % 16), then one
 // wave per group.  CHUNKS: regions in a lane's registers; 0: read again from LDS.
 template <int CHUNKS>
-__global__ __launch_bounds__(256) void region_pick_kernel(SelectArgs f, int NG, int stride)
+__global__ __launch_bounds__(PICK) void region_pick_kernel(SelectArgs f, int NG, int stride)
 {
     extern __shared__ uint64_t rank[];              // [NG][stride]
     const int G = f.q.m.regions, J = f.k.m.regions, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int per_head = (G + NG - 1) / NG;
     const int bm = blockIdx.x / per_head, i0 = (blockIdx.x - bm * per_head) * NG, b = bm / f.kv;
-    const int col = lane & 15, part = lane >> 4, run = f.dp >> 2;
+    const int col = lane & 15, part = lane >> 4;
     const int gi = min(i0 + min(col, NG - 1), G - 1);
-    const double* qp = f.q.sum + ((long long)bm * G + gi) * f.dp + part * run;
-    for (int j0 = 16 * wave; j0 < J; j0 += 64) {
+    const double* qp = f.q.sum + ((long long)bm * G + gi) * f.dp + 2 * part;
+    for (int j0 = 16 * wave; j0 < J; j0 += PICK / 4) {
         const int j = min(j0 + col, J - 1);
-        const double* kp = f.k.sum + ((long long)bm * J + j) * f.dp + part * run;
+        const double* kp = f.k.sum + ((long long)bm * J + j) * f.dp + 2 * part;
         d4 acc = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
-        for (int c = 0; c < run; c += 2) {
+        for (int c = 0; c < f.dp; c += 8) {
             const d2 x = *(const d2*)(qp + c), y = *(const d2*)(kp + c);
             acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[0], y[0], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[1], y[1], acc, 0, 0, 0);
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(256) void region_pick_kernel(SelectArgs f, int NG, 
             if (4 * r + part < NG) rank[(4 * r + part) * stride + j0 + col] = usable ? rank_of(acc[r]) : 0;
     }
     __syncthreads();
-    for (int n = wave; n < NG && i0 + n < G; n += 4) {
+    for (int n = wave; n < NG && i0 + n < G; n += PICK / 64) {
         int* list = f.index + ((long long)bm * G + i0 + n) * f.T;
         const bool any = f.q.count[(long long)b * G + i0 + n] > 0;
         const uint64_t* row = rank + n * stride;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(256) void region_pick_kernel(SelectArgs f, int NG, 
     }
 }
 
-static int padded(int d) { return (d + 7) & ~7; }           // (a quarter of it is whole pieces of two)
+static int padded(int d) { return (d + 7) & ~7; }           // (whole steps of two matrix instructions)
 
 struct SelectRoom { size_t q, k, nq, nk, end; };
 
@@ -251,7 +251,7 @@ static Side side_of(const Args& a, const void* x, const Strides& s, const Map& m
     o.units = o.pieces * o.together;
     const int lanes = POOL / o.units;
     o.lanes = 1;
-    while (o.lanes * 2 <= lanes && o.lanes < m.places) o.lanes *= 2;
+    while (o.lanes * 2 <= lanes && o.lanes * 8 < m.places * g) o.lanes *= 2;      // (eight loads or so for each thread)
     o.packed = lanes / o.lanes;
     o.head_blocks = (a.kv + o.together - 1) / o.together;
     o.blocks = a.B * ((m.regions + o.packed - 1) / o.packed) * o.head_blocks;
@@ -277,10 +277,10 @@ static hipError_t run(const Args& a, int* index, unsigned char* ws, hipStream_t 
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
 
-    // groups per block: 16 fill a matrix instruction; fewer where their ranks would leave room for one block in a compute unit
+    // groups per block: 16 fill a matrix instruction; fewer where their ranks would not let two blocks into a compute unit
     const int J = a.km.regions, stride = (J + 15) / 16 * 16 + 2;
     int NG = 16;
-    while (NG > 4 && NG * stride * 8 > 64 * 1024) NG /= 2;
+    while (NG > 4 && NG * stride * 8 > 80 * 1024) NG /= 2;
     while (NG > 1 && NG * stride * 8 > 144 * 1024) NG /= 2;
     const int blocks = a.B * a.kv * ((a.qm.regions + NG - 1) / NG), lds = NG * stride * 8;
     static LdsOptIn opt;
@@ -289,7 +289,7 @@ static hipError_t run(const Args& a, int* index, unsigned char* ws, hipStream_t 
     if (e != hipSuccess) return e;
     const auto kernel = J <= 64 ? region_pick_kernel<1> : J <= 128 ? region_pick_kernel<2> : J <= 256 ? region_pick_kernel<4>
                       : J <= 512 ? region_pick_kernel<8> : J <= 1024 ? region_pick_kernel<16> : region_pick_kernel<0>;
-    kernel<<<blocks, 256, lds, st>>>(f, NG, stride);
+    kernel<<<blocks, PICK, lds, st>>>(f, NG, stride);
     return hipGetLastError();
 }
 
