@@ -7,6 +7,7 @@ image evenly spaced in raster order.  A sequence [B, n, C] is passed as a map of
 stream of the tensors' device.
 """
 import ctypes
+import functools
 
 import torch
 
@@ -53,22 +54,16 @@ def _library():
 _CODES = {torch.float32: SLIDE_F32, torch.bfloat16: SLIDE_BF16}
 
 
-def _code(t):
-    if t.dtype not in _CODES:
-        raise SlideAttnError("activations must be float32 or bfloat16, got %s" % t.dtype)
-    return _CODES[t.dtype]
-
-
 def _int(value, name, lo, hi):
     if isinstance(value, bool) or not hasattr(value, "__index__") or not lo <= value.__index__() <= hi:
         raise SlideAttnError("%s must be an integer in [%d, %d]" % (name, lo, hi))
     return value.__index__()
 
 
-def _strides(t, name):
+def _strides(shape, stride, name):
     """Elements between the pixels and between the images of a [B, H, W, C] tensor."""
-    B, H, W, C = t.shape
-    sb, sh, sw, sc = t.stride()
+    B, H, W, C = shape
+    sb, sh, sw, sc = stride
     if W == 1:                                  # (strides of single elements say nothing)
         sw = sh if H > 1 else C
     if (C > 1 and sc != 1) or (H > 1 and sh != W * sw):
@@ -85,7 +80,7 @@ def _on(t, name, device):
 
 def _like(t, name, shape, dtype, device):
     """A tensor that must have this shape and type, and be contiguous."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise SlideAttnError("%s must be %s %s" % (name, str(dtype)[6:], list(shape)))
     _on(t, name, device)
     if not t.is_contiguous():
@@ -93,7 +88,8 @@ def _like(t, name, shape, dtype, device):
     return t.data_ptr()
 
 
-def _random(p, dropout, seed, offset, device):
+def _random(dropout, seed, offset, device):
+    """Rate, seed, number of the call, and where the rest of that number is read from on the device."""
     if not 0.0 <= dropout < 1.0 - 2.0 ** -17:
         raise SlideAttnError("dropout must be in [0, 1 - 2^-17)")
     number, holder = (0, offset) if isinstance(offset, torch.Tensor) else (_int(offset, "offset", 0, 2 ** 32 - 1), None)
@@ -104,87 +100,107 @@ def _random(p, dropout, seed, offset, device):
     return float(dropout), _int(seed, "seed", 0, 2 ** 64 - 1), number, None if holder is None else holder.data_ptr()
 
 
-def _problem(q, maps, heads, q_region, k_region, kv_heads, topk, q_size, k_size):
-    """The problem of maps q, k (and v), with everything checked that a kernel relies on."""
-    p = _Problem()
-    if q.dim() != 4:
-        raise SlideAttnError("activations must be [B, H, W, C]")
-    p.dtype = _code(q)
-    _on(q, "q", q.device)
-    p.B, p.q_h, p.q_w, channels = q.shape
-    p.heads = _int(heads, "heads", 1, 65535)
-    p.kv_heads = p.heads if kv_heads is None else _int(kv_heads, "kv_heads", 1, 65535)
-    if p.heads % p.kv_heads or channels % p.heads:
-        raise SlideAttnError("channels must be a multiple of heads, and heads of kv_heads")
-    p.head_dim = channels // p.heads
-    if not 1 <= p.head_dim <= 128:
-        raise SlideAttnError("head size must be 1..128")
-    shape = None
-    for name, t in maps:
-        if t.dim() != 4 or t.dtype != q.dtype or t.shape[0] != p.B or t.shape[3] != p.kv_heads * p.head_dim \
-                or t.shape != (shape or t.shape):
-            raise SlideAttnError("%s must be %s [%d, H, W, %d]%s" % (name, str(q.dtype)[6:], p.B, p.kv_heads * p.head_dim,
-                                                                   "" if shape is None else " as k is"))
-        shape = t.shape
-        _on(t, name, q.device)
-    p.k_h, p.k_w = shape[1], shape[2]
-    if min(p.B, p.q_h, p.q_w, p.k_h, p.k_w) < 1:
-        raise SlideAttnError("maps must not be empty")
-    p.q_pixel, p.q_image = _strides(q, "q")
-    p.k_pixel, p.k_image = _strides(maps[0][1], "k")
-    p.v_pixel, p.v_image = _strides(maps[1][1], "v") if len(maps) > 1 else (0, 0)
-    for name, region in (("q_region", q_region), ("k_region", k_region)):
-        if len(region) != 2:
-            raise SlideAttnError("%s must be (height, width)" % name)
-    p.q_region_h, p.q_region_w = (_int(n, "q_region", 1, 2 ** 31 - 1) for n in q_region)
-    p.k_region_h, p.k_region_w = (_int(n, "k_region", 1, 2 ** 31 - 1) for n in k_region)
-    p.topk = _int(topk, "topk", 1, 1024)
-    p.q_size = None if q_size is None else _like(q_size, "q_size", (p.B, 2), torch.int32, q.device)
-    p.k_size = None if k_size is None else _like(k_size, "k_size", (p.B, 2), torch.int32, q.device)
-    return p
+class _Plan:
+    """What follows from the sizes, strides and types of a call: its problem without pointers, the shapes of lists and lse, and
+    how much scratch each call needs on each device."""
 
+    def __init__(self, dtype, q_shape, q_stride, maps, heads, q_region, k_region, kv_heads, topk):
+        p = _Problem()
+        if len(q_shape) != 4:
+            raise SlideAttnError("activations must be [B, H, W, C]")
+        if dtype not in _CODES:
+            raise SlideAttnError("activations must be float32 or bfloat16, got %s" % dtype)
+        p.dtype = _CODES[dtype]
+        p.B, p.q_h, p.q_w, channels = q_shape
+        p.heads = _int(heads, "heads", 1, 65535)
+        p.kv_heads = p.heads if kv_heads is None else _int(kv_heads, "kv_heads", 1, 65535)
+        if p.heads % p.kv_heads or channels % p.heads:
+            raise SlideAttnError("channels must be a multiple of heads, and heads of kv_heads")
+        p.head_dim = channels // p.heads
+        if not 1 <= p.head_dim <= 128:
+            raise SlideAttnError("head size must be 1..128")
+        k_shape = maps[0][2]
+        for name, kind, shape, stride in maps:
+            if len(shape) != 4 or kind != dtype or shape[0] != p.B or shape[3] != p.kv_heads * p.head_dim or shape != k_shape:
+                raise SlideAttnError("%s must be %s [%d, H, W, %d]%s" % (name, str(dtype)[6:], p.B, p.kv_heads * p.head_dim,
+                                                                       "" if name == "k" else " as k is"))
+        p.k_h, p.k_w = k_shape[1], k_shape[2]
+        if min(p.B, p.q_h, p.q_w, p.k_h, p.k_w) < 1:
+            raise SlideAttnError("maps must not be empty")
+        p.q_pixel, p.q_image = _strides(q_shape, q_stride, "q")
+        p.k_pixel, p.k_image = _strides(k_shape, maps[0][3], "k")
+        p.v_pixel, p.v_image = _strides(k_shape, maps[1][3], "v") if len(maps) > 1 else (0, 0)
+        for name, region in (("q_region", q_region), ("k_region", k_region)):
+            if len(region) != 2:
+                raise SlideAttnError("%s must be (height, width)" % name)
+        p.q_region_h, p.q_region_w = (_int(n, "q_region", 1, 2 ** 31 - 1) for n in q_region)
+        p.k_region_h, p.k_region_w = (_int(n, "k_region", 1, 2 ** 31 - 1) for n in k_region)
+        p.topk = _int(topk, "topk", 1, 1024)
+        groups = -(-p.q_h // p.q_region_h) * -(-p.q_w // p.q_region_w)
+        self.image = bytes(p)
+        self.sizes = (p.B, 2)
+        self.lists = (p.B, p.kv_heads, groups, p.topk)
+        self.lse = (p.B, p.heads, p.q_h, p.q_w)
+        self.need = {}
 
-def _groups(p):
-    return -(-p.q_h // p.q_region_h) * -(-p.q_w // p.q_region_w)
+    def problem(self, q_size, k_size, device):
+        p = _Problem.from_buffer_copy(self.image)
+        if q_size is not None:
+            p.q_size = _like(q_size, "q_size", self.sizes, torch.int32, device)
+        if k_size is not None:
+            p.k_size = _like(k_size, "k_size", self.sizes, torch.int32, device)
+        return p
 
-
-class _On:
-    """The device of a call made current where it is not."""
-
-    def __init__(self, device):
-        self.index, self.guard = device.index, None
-        if torch.cuda.current_device() != self.index:
-            self.guard = torch.cuda.device(self.index)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return _stream(self.index)
-
-    def __exit__(self, *error):
-        if self.guard is not None:
-            self.guard.__exit__(*error)
-
-
-def _workspace(lib, p, call, workspace, like):
-    """Pointer and bytes of the scratch: the caller's, or as much as the call needs."""
-    if workspace is None:
-        need = lib.slide_region_workspace_bytes(p, call)
+    def scratch(self, p, call, workspace, like, index):
+        """Pointer and bytes of the scratch: the caller's, or as much as the call needs (its tensor last)."""
+        if workspace is not None:
+            _on(workspace, "workspace", like.device)
+            if not workspace.is_contiguous():
+                raise SlideAttnError("workspace must be contiguous")
+            return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+        need = self.need.get((call, index))
+        if need is None:
+            need = self.need[(call, index)] = _library().slide_region_workspace_bytes(p, call)
         if need == 0:
             return None, 0, None
         workspace = like.new_empty((need,), dtype=torch.uint8)
-    else:
-        _on(workspace, "workspace", like.device)
-        if not workspace.is_contiguous():
-            raise SlideAttnError("workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+        return workspace.data_ptr(), need, workspace
+
+
+_plan_of = functools.lru_cache(maxsize=4096)(_Plan)
+
+
+def _plan(q, maps, heads, q_region, k_region, kv_heads, topk):
+    """The plan of maps q, k (and v): everything that a kernel relies on is checked once per set of sizes, the devices every time."""
+    return _plan_of(q.dtype, q.shape, q.stride(), tuple((n, t.dtype, t.shape, t.stride()) for n, t in maps), heads,
+                    tuple(q_region), tuple(k_region), kv_heads, topk)
+
+
+def _device(q, maps):
+    device = q.device
+    if not q.is_cuda:
+        raise SlideAttnError("q must live on the GPU")
+    for n, t in maps:
+        if t.device != device:
+            _on(t, n, device)
+    return device
+
+
+def _enqueue(index, call):
+    """call(stream) with the device made current where it is not."""
+    if torch.cuda.current_device() == index:
+        return call(_stream(index))
+    with torch.cuda.device(index):
+        return call(_stream(index))
 
 
 def slide_region_workspace_bytes(call, q, k, topk, heads, q_region, k_region, kv_heads=None):
     """Bytes of scratch of slide_region_select ("select"), slide_region_attn_fwd ("fwd") or slide_region_attn_bwd ("bwd")."""
-    p = _problem(q, (("k", k), ("v", k)), heads, q_region, k_region, kv_heads, topk, None, None)
-    with _On(q.device):
-        return int(_library().slide_region_workspace_bytes(p, {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call]))
+    maps = (("k", k), ("v", k))
+    plan = _plan(q, maps, heads, q_region, k_region, kv_heads, topk)
+    p = plan.problem(None, None, _device(q, maps))
+    code = {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call]
+    return int(_enqueue(q.device.index, lambda stream: _library().slide_region_workspace_bytes(p, code)))
 
 
 def slide_region_select(q, k, topk, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None, index=None, workspace=None):
@@ -192,25 +208,35 @@ def slide_region_select(q, k, topk, heads, q_region, k_region, kv_heads=None, q_
 
     q_size, k_size: int32 [B, 2] tensors, the valid height and width of every image (None: the whole map)."""
     lib = _library()
-    p = _problem(q, (("k", k),), heads, q_region, k_region, kv_heads, topk, q_size, k_size)
-    shape = (p.B, p.kv_heads, _groups(p), p.topk)
-    with _On(q.device) as stream:
-        if index is None:
-            index = q.new_empty(shape, dtype=torch.int32)
-        ws, size, keep = _workspace(lib, p, _SELECT, workspace, q)
-        _check(lib.slide_region_select(p, q.data_ptr(), k.data_ptr(), _like(index, "index", shape, torch.int32, q.device), ws, size, stream))
-    return index
+    maps = (("k", k),)
+    plan = _plan(q, maps, heads, q_region, k_region, kv_heads, topk)
+    device = _device(q, maps)
+    p = plan.problem(q_size, k_size, device)
+
+    def call(stream):
+        lists = q.new_empty(plan.lists, dtype=torch.int32) if index is None else index
+        at = _like(lists, "index", plan.lists, torch.int32, device)
+        ws, size, keep = plan.scratch(p, _SELECT, workspace, q, device.index)
+        _check(lib.slide_region_select(p, q.data_ptr(), k.data_ptr(), at, ws, size, stream))
+        return lists
+
+    return _enqueue(device.index, call)
 
 
 def _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset):
+    """The plan, the problem with its pointers, and the lists of an attention call."""
     if index.dim() != 4:
         raise SlideAttnError("index must be int32 [B, kv_heads, regions of q, topk]")
-    p = _problem(q, (("k", k), ("v", v)), heads, q_region, k_region, kv_heads, index.shape[3], q_size, k_size)
-    p.dropout, p.seed, p.offset, p.offset_device = _random(p, dropout, seed, offset, q.device)
-    if scale is not None and not 0.0 < scale < float("inf"):
-        raise SlideAttnError("scale must be positive")
-    p.scale = 0.0 if scale is None else scale
-    return p, _like(index, "index", (p.B, p.kv_heads, _groups(p), p.topk), torch.int32, q.device)
+    maps = (("k", k), ("v", v))
+    plan = _plan(q, maps, heads, q_region, k_region, kv_heads, index.shape[3])
+    device = _device(q, maps)
+    p = plan.problem(q_size, k_size, device)
+    p.dropout, p.seed, p.offset, p.offset_device = _random(dropout, seed, offset, device)
+    if scale is not None:
+        if not 0.0 < scale < float("inf"):
+            raise SlideAttnError("scale must be positive")
+        p.scale = scale
+    return plan, p, _like(index, "index", plan.lists, torch.int32, device)
 
 
 def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None, scale=None,
@@ -220,29 +246,37 @@ def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=No
 
     dropout, seed, offset: of the attention weights; offset may be an int64 tensor with one element, read when the kernels run."""
     lib = _library()
-    p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
-    with _On(q.device) as stream:
-        out = q.new_empty(q.shape) if out is None else out
-        out_at = _like(out, "out", q.shape, q.dtype, q.device)
-        lse_at = None if lse is None else _like(lse, "lse", (p.B, p.heads, p.q_h, p.q_w), torch.float32, q.device)
-        ws, size, keep = _workspace(lib, p, _FWD, workspace, q)
+    plan, p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
+    device = q.device
+
+    def call(stream):
+        result = q.new_empty(q.shape) if out is None else out
+        out_at = _like(result, "out", q.shape, q.dtype, device)
+        lse_at = None if lse is None else _like(lse, "lse", plan.lse, torch.float32, device)
+        ws, size, keep = plan.scratch(p, _FWD, workspace, q, device.index)
         _check(lib.slide_region_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, out_at, lse_at, ws, size, stream))
-    return out
+        return result
+
+    return _enqueue(device.index, call)
 
 
 def slide_region_attn_bwd(dout, q, k, v, index, out, lse, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None,
                           scale=None, dropout=0.0, seed=0, offset=0, outputs=None, workspace=None):
     """Returns (dq, dk, dv), contiguous.  out, lse: the forward's results for the same arguments."""
     lib = _library()
-    p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
-    with _On(q.device) as stream:
+    plan, p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
+    device = q.device
+
+    def call(stream):
         dq, dk, dv = (q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)) if outputs is None else outputs
-        at = [_like(t, name, like.shape, q.dtype, q.device)
+        at = [_like(t, name, like.shape, q.dtype, device)
               for t, name, like in ((dout, "dout", q), (out, "out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
-        lse_at = _like(lse, "lse", (p.B, p.heads, p.q_h, p.q_w), torch.float32, q.device)
-        ws, size, keep = _workspace(lib, p, _BWD, workspace, q)
+        lse_at = _like(lse, "lse", plan.lse, torch.float32, device)
+        ws, size, keep = plan.scratch(p, _BWD, workspace, q, device.index)
         _check(lib.slide_region_attn_bwd(p, at[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, at[1], lse_at, *at[2:], ws, size, stream))
-    return dq, dk, dv
+        return dq, dk, dv
+
+    return _enqueue(device.index, call)
 
 
 def _dropout(entry, x, name, residual, p, seed, offset, y):
@@ -250,17 +284,20 @@ def _dropout(entry, x, name, residual, p, seed, offset, y):
         raise SlideAttnError("%s must live on the GPU" % name)
     if not x.is_contiguous():
         raise SlideAttnError("%s must be contiguous" % name)
-    code = _code(x)
-    p, seed, number, holder = _random(None, p, seed, offset, x.device)
-    with _On(x.device) as stream:
-        y = x.new_empty(x.shape) if y is None else y
-        y_at = _like(y, "the result", x.shape, x.dtype, x.device)
-        at = (x.data_ptr(),)
+    if x.dtype not in _CODES:
+        raise SlideAttnError("%s must be float32 or bfloat16, got %s" % (name, x.dtype))
+    p, seed, number, holder = _random(p, seed, offset, x.device)
+
+    def call(stream):
+        result = x.new_empty(x.shape) if y is None else y
+        at = (_like(result, "the result", x.shape, x.dtype, x.device),)
         if residual is not False:
-            at += (None if residual is None else _like(residual, "residual", x.shape, x.dtype, x.device),)
+            at = (None if residual is None else _like(residual, "residual", x.shape, x.dtype, x.device),) + at
         if x.numel():
-            _check(entry(*at, y_at, x.numel(), code, p, seed, number, holder, stream))
-    return y
+            _check(entry(x.data_ptr(), *at, x.numel(), _CODES[x.dtype], p, seed, number, holder, stream))
+        return result
+
+    return _enqueue(x.device.index, call)
 
 
 def slide_dropout_fwd(x, p, seed, offset=0, residual=None, out=None):

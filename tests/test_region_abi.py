@@ -120,7 +120,9 @@ def test_binding_names_what_is_wrong():
 
 
 def test_strides_of_parts():
-    strides = region._strides
+    def strides(t, name):
+        return region._strides(t.shape, t.stride(), name)
+
     x = torch.zeros(2, 4, 5, 96)
     assert strides(x, "x") == (96, 96 * 20)
     assert strides(x[..., 32:64], "x") == (96, 96 * 20)                     # a part of the channels
