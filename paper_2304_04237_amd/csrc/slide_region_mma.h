@@ -19,6 +19,12 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+// two floats rounded to bf16 (to nearest, ties to even) in one dword: one instruction
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, bf2)); }
+
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // row that register r of a product's result is in lane half h
@@ -119,7 +125,7 @@ template <> struct Weights<bf16_bits> {
     __device__ __forceinline__ void set(const f16v& p)
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = (uint32_t)f32_to_bf16(p[2 * i]) | (uint32_t)f32_to_bf16(p[2 * i + 1]) << 16;
+        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = pack_bf16(p[2 * i], p[2 * i + 1]);
     }
 };
 template <> struct Weights<float> {
@@ -191,7 +197,7 @@ __device__ __forceinline__ void store4(bf16_bits* p, const float (&x)[4], int le
 {
     if (vec) {
         if (left > 0)
-            *(u2*)p = u2{(uint32_t)f32_to_bf16(x[0]) | (uint32_t)f32_to_bf16(x[1]) << 16, (uint32_t)f32_to_bf16(x[2]) | (uint32_t)f32_to_bf16(x[3]) << 16};
+            *(u2*)p = u2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
