@@ -200,33 +200,43 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
     }
 }
 
-// The lists turned around: one wave per region of keys goes over all entries of its image and head.
+// The lists turned around: a block per region of keys goes over all entries of its image and head, each wave over a quarter of them,
+// first counting, then writing in order.
 __global__ __launch_bounds__(256) void region_invert_kernel(BwdArgs f)
 {
     const Args& a = f.a;
-    const int lane = threadIdx.x & 63;
-    const long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int J = a.km.regions;
-    if (id >= (long long)a.B * a.kv * J) return;
-    const int bm = (int)(id / J), j = (int)(id - (long long)bm * J);
+    __shared__ int2 counts[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, J = a.km.regions;
+    const int bm = blockIdx.x / J, j = blockIdx.x - bm * J;
     const int* list = a.index + (long long)bm * f.entries;
+    const int run = (f.entries + 255) / 256 * 64, first = min(wave * run, f.entries), end = min(first + run, f.entries);
     int less = 0, mine = 0;
-    for (int e = lane; e < f.entries; e += 64) {
+#pragma unroll 8
+    for (int e = first + lane; e < end; e += 64) {
         const int x = list[e];
         less += x >= 0 && x < j;
         mine += x == j;
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) { less += __shfl_xor(less, s); mine += __shfl_xor(mine, s); }
-    if (lane == 0) {
-        f.start[(long long)bm * (J + 1) + j] = less;
-        if (j == J - 1) f.start[(long long)bm * (J + 1) + J] = less + mine;
+    if (lane == 0) counts[wave] = int2{less, mine};
+    __syncthreads();
+    int at = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        at += counts[w].x + (w < wave ? counts[w].y : 0);
+        total += counts[w].y;
     }
-    if (mine == 0) return;
-    int2* to = f.sorted + (long long)bm * f.entries + less;
-    for (int e0 = 0; e0 < f.entries; e0 += 64) {
+    if (threadIdx.x == 0) {
+        f.start[(long long)bm * (J + 1) + j] = at;
+        if (j == J - 1) f.start[(long long)bm * (J + 1) + J] = at + total;
+    }
+    if (counts[wave].y == 0) return;
+    int2* to = f.sorted + (long long)bm * f.entries + at;
+#pragma unroll 4
+    for (int e0 = first; e0 < end; e0 += 64) {
         const int e = e0 + lane;
-        const bool hit = e < f.entries && list[e] == j;
+        const bool hit = e < end && list[e] == j;
         const uint64_t mask = __ballot(hit);
         if (hit) to[__popcll(mask & ((1ull << lane) - 1))] = int2{e / a.T, j};
         to += __popcll(mask);
@@ -546,7 +556,7 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
     if (two_tiles<T>(a, a.R)) e = run_rows<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
     else e = a.d <= 32 ? run_rows<T, 32, 1>(f, st) : a.d <= 64 ? run_rows<T, 64, 1>(f, st) : run_rows<T, 128, 1>(f, st);
     if (e != hipSuccess) return e;
-    region_invert_kernel<<<(int)(((long long)a.B * a.kv * a.km.regions + 3) / 4), 256, 0, st>>>(f);
+    region_invert_kernel<<<a.B * a.kv * a.km.regions, 256, 0, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (two_tiles<T>(a, a.km.places)) return run_keys<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
     return a.d <= 32 ? run_keys<T, 32, 1>(f, st) : a.d <= 64 ? run_keys<T, 64, 1>(f, st) : run_keys<T, 128, 1>(f, st);

@@ -96,9 +96,18 @@ __device__ __forceinline__ f16v dot(const Operand<float, D>& a, const Operand<fl
     return acc;
 }
 
-// A tile of 32 pixels x D channels in LDS that this wave alone uses
+// A tile of 32 pixels x D channels in LDS that this wave alone uses.  The 16-byte pieces of a row are exchanged by a number that the
+// row gives, so that neither eight rows' writes of one piece nor a transposing read of four rows meet in a bank.
 template <typename T, int D> struct Tile {
     static constexpr int BYTES = 32 * D * (int)sizeof(T);
+    static __device__ __forceinline__ int exchange(int row)
+    {
+        if constexpr (sizeof(T) == 4) return row & 7;
+        else if constexpr (D == 32) return (row & 2) | ((row >> 2) & 1);        // (two rows in 128 bytes)
+        else return 2 * (row & 3) | ((row >> 2) & 1);
+    }
+    // byte of piece c of a row
+    static __device__ __forceinline__ int at(int row, int c) { return row * D * (int)sizeof(T) + ((c ^ exchange(row)) << 4); }
 };
 
 // the pieces of a lane (pixel lane % 32, half of the pieces) into the tile
@@ -107,14 +116,14 @@ __device__ __forceinline__ void stage(unsigned char* tile, const Operand<bf16_bi
 {
     const int row = lane & 31, h = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) *(u4*)(tile + row * D * 2 + (2 * i + h) * 16) = o.v[i];
+    for (int i = 0; i < D / 16; ++i) *(u4*)(tile + Tile<bf16_bits, D>::at(row, 2 * i + h)) = o.v[i];
 }
 template <int D>
 __device__ __forceinline__ void stage(unsigned char* tile, const Operand<float, D>& o, int lane)
 {
     const int row = lane & 31, h = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) *(f4*)(tile + (row * D + h * (D / 2) + 4 * i) * 4) = o.v[i];
+    for (int i = 0; i < D / 8; ++i) *(f4*)(tile + Tile<float, D>::at(row, h * (D / 8) + i)) = o.v[i];
 }
 
 // Weights of 32 rows (registers of a product's result) as a right operand
@@ -140,7 +149,7 @@ __device__ __forceinline__ void read_transposed(u4 (&a)[2], const unsigned char*
     const int s = lane & 15, h = lane >> 5, dh = (lane >> 4) & 1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const unsigned char* p = tile + (8 * i + 4 * h + (s >> 2)) * D * 2 + (32 * dt + 16 * dh + 4 * (s & 3)) * 2;
+        const unsigned char* p = tile + Tile<bf16_bits, D>::at(8 * i + 4 * h + (s >> 2), 4 * dt + 2 * dh + ((s >> 1) & 1)) + 8 * (s & 1);
         const u2 x = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)p));
         a[i >> 1][2 * (i & 1)] = x[0];
         a[i >> 1][2 * (i & 1) + 1] = x[1];
@@ -165,13 +174,12 @@ __device__ __forceinline__ void accumulate(f16v (&acc)[NC][D / 32], const unsign
 template <int D, int NC>
 __device__ __forceinline__ void accumulate(f16v (&acc)[NC][D / 32], const unsigned char* tile, const Weights<float> (&w)[NC], int lane)
 {
-    const float* t = (const float*)tile + (lane & 31);
     const int h = lane >> 5;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const float a = t[acc_row(r, h) * D + 32 * dt];
+            const float a = *(const float*)(tile + Tile<float, D>::at(acc_row(r, h), 8 * dt + ((lane & 31) >> 2)) + 4 * (lane & 3));
 #pragma unroll
             for (int c = 0; c < NC; ++c) acc[c][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[c].v[r], acc[c][dt], 0, 0, 0);
         }
