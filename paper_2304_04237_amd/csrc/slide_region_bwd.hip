@@ -5,7 +5,7 @@
 //   dk = scale sum dS q,  dv = sum F P dout   (key kernel: a wave per 32 NK keys of a region, over the rows of the groups that list it)
 //
 // Between the two a kernel turns the lists around (which groups list region j, in ascending order, so that sums have one order).
-// A wave takes at most `share` of a region's groups; what is beyond goes to further waves, whose float32 sums a last kernel adds up.
+// A block takes at most `share` of a region's groups; what is beyond goes to further blocks, whose float32 sums a last kernel adds up.
 #include "slide_region_mma.h"
 
 namespace slide {
@@ -26,9 +26,11 @@ struct BwdArgs {
     float* partial;         // [B * kv][key tiles][2 windows][2][32 NK][D]
     int slots, tiles, row_tiles, key_tiles, items;
     int entries;            // regions of q * T
-    int share, windows;     // entries per wave, ceil(entries / share)
+    int share, windows;     // entries per block of the key kernel, ceil(entries / share)
+    int team;               // waves that share a tile of keys, 1 or 4
+    int invert_waves;       // waves per region in the inversion, 1 or 4
     Div by_row_tiles;
-    int vec_q, vec_k, vec_v, vec_do, vec_o, vec_dq, vec_dk;
+    int vec, vec_dq, vec_dk;        // inputs in whole 16-byte pieces; dq, dk and dv in whole quads
 };
 
 template <typename T> __device__ __forceinline__ float piece_dot(const u4& a, const u4& b);
@@ -53,7 +55,7 @@ template <> __device__ __forceinline__ float piece_dot<float>(const u4& a, const
 // dq and, for the key kernel, every row's lse and D.
 // bf16: out was rounded, so dout.out is off by up to 2^-8 of its terms.  The sum of P F dP, which is D without that, is only known at
 // the end; until then the rounded D0 is used, and dq is corrected by (D - D0) sum P k, for one more product.
-template <typename T, int D, int NR, bool DROP>
+template <typename T, int D, int NR, bool DROP, bool VEC>
 __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
 {
     constexpr bool FIX = sizeof(T) == 2;
@@ -83,10 +85,10 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
             const long long n_px = (long long)a.qm.H * a.qm.W;
             out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
             const long long at = ok ? out_at[n] : 0;
-            load_operand<T, D>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h, f.vec_q);
-            load_operand<T, D>(g[n], (const T*)f.dout + at, ok, a.d, h, f.vec_do);
+            load_operand<T, D, VEC>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h);
+            load_operand<T, D, VEC>(g[n], (const T*)f.dout + at, ok, a.d, h);
             Operand<T, D> o;
-            load_operand<T, D>(o, (const T*)f.out + at, ok, a.d, h, f.vec_o);
+            load_operand<T, D, VEC>(o, (const T*)f.out + at, ok, a.d, h);
             float s = 0.0f;
 #pragma unroll
             for (int u = 0; u < (int)(sizeof(o) / 16); ++u)
@@ -118,8 +120,8 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
         next_ok = (uint32_t)__ballot(px >= 0);
         if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
-        load_operand<T, D>(kn, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h, f.vec_k);
-        load_operand<T, D>(vn, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h, f.vec_v);
+        load_operand<T, D, VEC>(kn, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h);
+        load_operand<T, D, VEC>(vn, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h);
     };
     fetch();
     region = walk.look(a, 32 + col, f.slots);
@@ -200,16 +202,20 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
     }
 }
 
-// The lists turned around: a block per region of keys goes over all entries of its image and head, each wave over a quarter of them,
-// first counting, then writing in order.
+// The lists turned around: a wave per region of keys (or four, each over a quarter, where the lists are long) goes over
+// all entries of its image and head, first counting, then writing in order.
 __global__ __launch_bounds__(256) void region_invert_kernel(BwdArgs f)
 {
     const Args& a = f.a;
     __shared__ int2 counts[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, J = a.km.regions;
-    const int bm = blockIdx.x / J, j = blockIdx.x - bm * J;
+    const int lane = threadIdx.x & 63, J = a.km.regions;
+    const int waves = f.invert_waves, wave = (threadIdx.x >> 6) & (waves - 1), base = (threadIdx.x >> 6) - wave;
+    const long long id = (long long)blockIdx.x * (4 / waves) + base / waves;
+    const bool live = id < (long long)a.B * a.kv * J;
+    const int bm = live ? (int)(id / J) : 0, j = live ? (int)(id - (long long)bm * J) : -1;
     const int* list = a.index + (long long)bm * f.entries;
-    const int run = (f.entries + 255) / 256 * 64, first = min(wave * run, f.entries), end = min(first + run, f.entries);
+    const int run = (f.entries + 64 * waves - 1) / (64 * waves) * 64;
+    const int first = min(wave * run, f.entries), end = live ? min(first + run, f.entries) : 0;
     int less = 0, mine = 0;
 #pragma unroll 8
     for (int e = first + lane; e < end; e += 64) {
@@ -219,19 +225,19 @@ __global__ __launch_bounds__(256) void region_invert_kernel(BwdArgs f)
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) { less += __shfl_xor(less, s); mine += __shfl_xor(mine, s); }
-    if (lane == 0) counts[wave] = int2{less, mine};
+    if (lane == 0) counts[base + wave] = int2{less, mine};
     __syncthreads();
+    if (!live) return;
     int at = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        at += counts[w].x + (w < wave ? counts[w].y : 0);
-        total += counts[w].y;
+    for (int w = 0; w < waves; ++w) {
+        at += counts[base + w].x + (w < wave ? counts[base + w].y : 0);
+        total += counts[base + w].y;
     }
-    if (threadIdx.x == 0) {
+    if (wave == 0 && lane == 0) {
         f.start[(long long)bm * (J + 1) + j] = at;
         if (j == J - 1) f.start[(long long)bm * (J + 1) + J] = at + total;
     }
-    if (counts[wave].y == 0) return;
+    if (counts[base + wave].y == 0) return;
     int2* to = f.sorted + (long long)bm * f.entries + at;
 #pragma unroll 4
     for (int e0 = first; e0 < end; e0 += 64) {
@@ -269,22 +275,20 @@ __device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint3
     pairs(std::integral_constant<int, 2>{}); pairs(std::integral_constant<int, 3>{});
 }
 
-// dk and dv of 32 NK keys of a region.
-template <typename T, int D, int NK, bool DROP>
-__global__ __launch_bounds__(256) void region_dkdv_kernel(BwdArgs f)
+// dk and dv of 32 NK keys of a region, by one wave or a team of four that divide the entries among them and add their sums in LDS.
+template <typename T, int D, int NK, bool DROP, int TEAM, bool VEC>
+__global__ __launch_bounds__(64 * TEAM) void region_dkdv_kernel(BwdArgs f)
 {
     const Args& a = f.a;
     extern __shared__ __align__(16) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int item = (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
-    if (item >= f.items) return;
-    constexpr int ROOM = 2 * Tile<T, D>::BYTES + 256;
-    unsigned char* tile_q = lds + wave * ROOM;
+    const int lane = threadIdx.x & 63, wave = TEAM == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int item = (int)xcd_order(blockIdx.x, gridDim.x);
+    unsigned char* tile_q = lds + wave * (2 * Tile<T, D>::BYTES + 256);
     unsigned char* tile_g = tile_q + Tile<T, D>::BYTES;
     float* stat = (float*)(tile_g + Tile<T, D>::BYTES);        // lse, then D, of 32 rows
     const int J = a.km.regions, col = lane & 31, h = lane >> 5;
 
-    // this wave's work: the first `share` entries of a region (units 0 .. J - 1), or those of a window that lie beyond (the rest)
+    // this block's work: the first `share` entries of a region (units 0 .. J - 1), or those of a window that lie beyond (the rest)
     const int per_image = (J + f.windows) * f.key_tiles;
     const int bm = item / per_image;
     int unit = item - bm * per_image;
@@ -310,6 +314,11 @@ __global__ __launch_bounds__(256) void region_dkdv_kernel(BwdArgs f)
     }
     j = __builtin_amdgcn_readfirstlane(j); from = __builtin_amdgcn_readfirstlane(from); to = __builtin_amdgcn_readfirstlane(to);
     slot = __builtin_amdgcn_readfirstlane(slot);
+    if (TEAM > 1) {
+        const int n = to - from, mine = (int)((long long)n * wave / TEAM);
+        to = from + (int)((long long)n * (wave + 1) / TEAM);
+        from += mine;
+    }
 
     Operand<T, D> k[NK], v[NK];
     long long out_at[NK];
@@ -327,8 +336,8 @@ __global__ __launch_bounds__(256) void region_dkdv_kernel(BwdArgs f)
             out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.kv * a.d + m * a.d;
             quad[n] = (uint32_t)j * a.quads + (place >> 2);
             const long long at = valid[n] ? px : 0;
-            load_operand<T, D>(k[n], (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.d, valid[n], a.d, h, f.vec_k);
-            load_operand<T, D>(v[n], (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.d, valid[n], a.d, h, f.vec_v);
+            load_operand<T, D, VEC>(k[n], (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.d, valid[n], a.d, h);
+            load_operand<T, D, VEC>(v[n], (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.d, valid[n], a.d, h);
         }
     }
     const uint32_t call = DROP ? a.rnd.call() : 0;
@@ -352,8 +361,8 @@ __global__ __launch_bounds__(256) void region_dkdv_kernel(BwdArgs f)
         const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
         const int px = r < a.R ? a.qm.pixel(i, place, qh, qw) : -1;
         const bool ok = px >= 0;
-        load_operand<T, D>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h, f.vec_q);
-        load_operand<T, D>(g, (const T*)f.dout + (ok ? ((long long)b * n_px + px) * a.heads * a.d + head * a.d : 0), ok, a.d, h, f.vec_do);
+        load_operand<T, D, VEC>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h);
+        load_operand<T, D, VEC>(g, (const T*)f.dout + (ok ? ((long long)b * n_px + px) * a.heads * a.d + head * a.d : 0), ok, a.d, h);
         st = (h ? f.row_D : f.row_lse)[((long long)bm * a.qm.regions + i) * f.row_tiles * 32 + r];
     };
     int next = group_of(0), i = next;
@@ -402,6 +411,41 @@ __global__ __launch_bounds__(256) void region_dkdv_kernel(BwdArgs f)
         accumulate<D, NK>(dk, tile_q, wk, lane);
     }
 
+    if constexpr (TEAM > 1) {
+        // waves 2 and 3 hand their sums to 0 and 1, then 1 to 0; a lane's registers stay its own
+        static_assert(TEAM == 4, "two rounds");
+        float* room = (float*)lds + lane;
+        constexpr int N = 2 * NK * (D / 32) * 16;
+#pragma unroll
+        for (int half = 2; half > 0; half >>= 1) {
+            __syncthreads();
+            float* to_lds = room + (wave & (half - 1)) * N * 64;
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (int n = 0; n < NK; ++n)
+#pragma unroll
+                    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            to_lds[((n * (D / 32) + dt) * 32 + r) * 64] = dk[n][dt][r];
+                            to_lds[((n * (D / 32) + dt) * 32 + 16 + r) * 64] = dv[n][dt][r];
+                        }
+            }
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (int n = 0; n < NK; ++n)
+#pragma unroll
+                    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            dk[n][dt][r] += to_lds[((n * (D / 32) + dt) * 32 + r) * 64];
+                            dv[n][dt][r] += to_lds[((n * (D / 32) + dt) * 32 + 16 + r) * 64];
+                        }
+            }
+        }
+        if (wave > 0) return;
+    }
     float* part = f.partial + (((long long)bm * f.key_tiles + kt) * 2 * f.windows + max(slot, 0)) * (2 * 32 * NK * D);
 #pragma unroll
     for (int n = 0; n < NK; ++n)
@@ -456,7 +500,7 @@ __global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
 
 // Two row tiles (or tiles of keys) per wave halve the reads of the other side's operands, where the registers hold them: the
 // sums take 2 x 16 registers per tile and 32 channels.
-template <typename T> static bool two_tiles(const Args& a, int n) { return sizeof(T) == 2 && a.d <= 32 && n > 32; }
+template <typename T> static bool two_tiles(const BwdArgs& f, int n) { return sizeof(T) == 2 && f.a.d <= 32 && n > 32 && f.vec; }
 
 static int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
@@ -467,12 +511,15 @@ template <typename T> static void plan(BwdArgs& f)
     f.slots = 4 * a.quads * a.T;
     f.row_tiles = (a.R + 31) / 32;
     f.by_row_tiles = Div::by(f.row_tiles);
-    f.key_tiles = (a.km.places + (two_tiles<T>(a, a.km.places) ? 63 : 31)) / (two_tiles<T>(a, a.km.places) ? 64 : 32);
+    f.key_tiles = (a.km.places + (two_tiles<T>(f, a.km.places) ? 63 : 31)) / (two_tiles<T>(f, a.km.places) ? 64 : 32);
     f.entries = a.qm.regions * a.T;
-    // A wave's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip
+    // Four waves per tile of keys where a region has 24 row tiles or more on average (16384 tokens, 128 row tiles per region: 155
+    // against 218 us); with few, as at stage 1 (8), the joining costs more than the finer division gives.
     const long long average = ((long long)f.entries + a.km.regions - 1) / a.km.regions;
-    const long long all = (long long)a.B * a.kv * f.key_tiles * f.entries;
-    const long long fill = std::max(1ll, all / (8ll * device_cu_count()));
+    f.team = average * f.row_tiles >= 24 ? 4 : 1;
+    // A block's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip
+    const long long all = (long long)a.B * a.kv * f.key_tiles * f.entries * f.team;
+    const long long fill = std::max((long long)f.team, all / (16ll * device_cu_count()));
     f.share = (int)std::min(std::max(2 * average, (8ll + f.row_tiles - 1) / f.row_tiles), fill);
     f.windows = (f.entries + f.share - 1) / f.share;
 }
@@ -484,7 +531,7 @@ template <typename T> static Room room(const BwdArgs& f)
     const Args& a = f.a;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     const size_t bm = (size_t)a.B * a.kv, rows = bm * a.qm.regions * f.row_tiles * 32 * sizeof(float);
-    const int nk = two_tiles<T>(a, a.km.places) ? 2 : 1;
+    const int nk = two_tiles<T>(f, a.km.places) ? 2 : 1;
     Room r;
     r.lse = 0;
     r.D = up(rows);
@@ -497,10 +544,15 @@ template <typename T> static Room room(const BwdArgs& f)
 
 template <typename T> static size_t bytes_t(const Args& a)
 {
-    BwdArgs f{};
-    f.a = a;
-    plan<T>(f);
-    return room<T>(f).end;
+    size_t most = 0;                        // (whether the inputs come in whole pieces is known at the call only)
+    for (int vec = 0; vec < 2; ++vec) {
+        BwdArgs f{};
+        f.a = a;
+        f.vec = vec;
+        plan<T>(f);
+        most = std::max(most, room<T>(f).end);
+    }
+    return most;
 }
 
 size_t bwd_workspace_bytes(const Args& a) { return a.dtype == 0 ? bytes_t<float>(a) : bytes_t<bf16_bits>(a); }
@@ -511,8 +563,10 @@ static hipError_t run_rows(BwdArgs& f, hipStream_t st)
     f.tiles = (f.a.R + 32 * NR - 1) / (32 * NR);
     f.items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
     const int blocks = (f.items + 3) / 4, lds = 4 * Tile<T, D>::BYTES;
-    if (f.a.rnd.threshold) region_dq_kernel<T, D, NR, true><<<blocks, 256, lds, st>>>(f);
-    else region_dq_kernel<T, D, NR, false><<<blocks, 256, lds, st>>>(f);
+    // (what is not in whole pieces takes the kernels with dropout, which drop nothing below a threshold of 0)
+    const auto kernel = !f.vec ? region_dq_kernel<T, D, 1, true, false>
+                      : f.a.rnd.threshold ? region_dq_kernel<T, D, NR, true, true> : region_dq_kernel<T, D, NR, false, true>;
+    kernel<<<blocks, 256, lds, st>>>(f);
     return hipGetLastError();
 }
 
@@ -520,14 +574,18 @@ template <typename T, int D, int NK>
 static hipError_t run_keys(BwdArgs& f, hipStream_t st)
 {
     const long long items = (long long)f.a.B * f.a.kv * f.key_tiles * (f.a.km.regions + f.windows);
-    f.items = (int)items;
-    const int blocks = (f.items + 3) / 4, lds = 4 * (2 * Tile<T, D>::BYTES + 256);
+    const int one = 2 * Tile<T, D>::BYTES + 256, lds = f.team == 1 ? one : std::max(4 * one, 2 * 2 * NK * D * 32 * 4);
     static LdsOptIn opt;
-    hipError_t e = opt.ensure({(const void*)region_dkdv_kernel<T, D, NK, true>, (const void*)region_dkdv_kernel<T, D, NK, false>}, lds);
+    hipError_t e = opt.ensure({(const void*)region_dkdv_kernel<T, D, NK, true, 4, true>, (const void*)region_dkdv_kernel<T, D, NK, false, 4, true>,
+                               (const void*)region_dkdv_kernel<T, D, 1, true, 4, false>}, 4 * one);
     if (e != hipSuccess) return e;
-    if (f.a.rnd.threshold) region_dkdv_kernel<T, D, NK, true><<<blocks, 256, lds, st>>>(f);
-    else region_dkdv_kernel<T, D, NK, false><<<blocks, 256, lds, st>>>(f);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const bool team = f.team > 1;
+    const auto kernel = !f.vec ? (team ? region_dkdv_kernel<T, D, 1, true, 4, false> : region_dkdv_kernel<T, D, 1, true, 1, false>)
+                      : f.a.rnd.threshold ? (team ? region_dkdv_kernel<T, D, NK, true, 4, true> : region_dkdv_kernel<T, D, NK, true, 1, true>)
+                                          : (team ? region_dkdv_kernel<T, D, NK, false, 4, true> : region_dkdv_kernel<T, D, NK, false, 1, true>);
+    kernel<<<(int)items, 64 * f.team, lds, st>>>(f);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
     if (f.entries > f.share) {
         region_dkdv_join_kernel<T, D, NK><<<f.a.B * f.a.kv * f.key_tiles * f.windows, 256, 0, st>>>(f);
         e = hipGetLastError();
@@ -539,26 +597,24 @@ template <typename T>
 static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
 {
     const Args& a = f.a;
+    const Strides whole{(long long)a.heads * a.d, (long long)a.qm.H * a.qm.W * a.heads * a.d};
+    f.vec = pieces(a.q, a.qs, a.d, sizeof(T)) && pieces(a.k, a.ks, a.d, sizeof(T)) && pieces(a.v, a.vs, a.d, sizeof(T)) &&
+            pieces(f.dout, whole, a.d, sizeof(T)) && pieces(f.out, whole, a.d, sizeof(T));
     plan<T>(f);
     const Room r = room<T>(f);
     f.row_lse = (float*)(ws + r.lse); f.row_D = (float*)(ws + r.D); f.sorted = (int2*)(ws + r.sorted);
     f.start = (int*)(ws + r.start); f.partial = (float*)(ws + r.partial);
-    const Strides whole{(long long)a.heads * a.d, (long long)a.qm.H * a.qm.W * a.heads * a.d};
-    f.vec_q = pieces(a.q, a.qs, a.d, sizeof(T));
-    f.vec_k = pieces(a.k, a.ks, a.d, sizeof(T));
-    f.vec_v = pieces(a.v, a.vs, a.d, sizeof(T));
-    f.vec_do = pieces(f.dout, whole, a.d, sizeof(T));
-    f.vec_o = pieces(f.out, whole, a.d, sizeof(T));
     const uintptr_t quad = 4 * sizeof(T) - 1;
     f.vec_dq = a.d % 4 == 0 && ((uintptr_t)f.dq & quad) == 0;
     f.vec_dk = a.d % 4 == 0 && ((uintptr_t)f.dk & quad) == 0 && ((uintptr_t)f.dv & quad) == 0;
     hipError_t e;
-    if (two_tiles<T>(a, a.R)) e = run_rows<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
+    if (two_tiles<T>(f, a.R)) e = run_rows<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
     else e = a.d <= 32 ? run_rows<T, 32, 1>(f, st) : a.d <= 64 ? run_rows<T, 64, 1>(f, st) : run_rows<T, 128, 1>(f, st);
     if (e != hipSuccess) return e;
-    region_invert_kernel<<<a.B * a.kv * a.km.regions, 256, 0, st>>>(f);
+    f.invert_waves = f.entries >= 2048 ? 4 : 1;         // (196 entries: 5.5 us by one, 8.3 by four; 16384: 109 by one, 18 by four)
+    region_invert_kernel<<<(int)(((long long)a.B * a.kv * a.km.regions * f.invert_waves + 3) / 4), 256, 0, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (two_tiles<T>(a, a.km.places)) return run_keys<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
+    if (two_tiles<T>(f, a.km.places)) return run_keys<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
     return a.d <= 32 ? run_keys<T, 32, 1>(f, st) : a.d <= 64 ? run_keys<T, 64, 1>(f, st) : run_keys<T, 128, 1>(f, st);
 }
 

@@ -20,7 +20,7 @@ struct FwdArgs {
     float* lse;
     int tiles;              // of 32 NR rows in a group
     int slots;              // keys of a group, with every listed region's slots a multiple of 4
-    int vec_q, vec_k, vec_v, vec_o;
+    int vec, vec_o;         // q, k, v in whole 16-byte pieces; out in whole quads
     int items;              // waves (SPLIT: blocks) with work
     int shares;             // SPLIT: blocks that share the keys of 32 rows
     float* part;            // SPLIT, shares > 1: [rows' item][share][32][D] sums, then [2][32] maxima and sums
@@ -34,7 +34,7 @@ __device__ __forceinline__ void finish(const FwdArgs& f, long long out_at, int c
     store4((T*)f.out + out_at + c, x, f.a.d - c, f.vec_o);
 }
 
-template <typename T, int D, int NR, bool DROP, bool SPLIT>
+template <typename T, int D, int NR, bool DROP, bool SPLIT, bool VEC>
 __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
 {
     const Args& a = f.a;
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
             const long long n_px = (long long)a.qm.H * a.qm.W;
             out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
             lse_at[n] = px < 0 ? -1 : (((long long)b * a.heads + head) * n_px + px) * 2 + ok;      // (lowest bit: the row is valid)
-            load_operand<T, D>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px : 0) * a.qs.pixel + head * a.d, ok, a.d, h, f.vec_q);
+            load_operand<T, D, VEC>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px : 0) * a.qs.pixel + head * a.d, ok, a.d, h);
         }
     }
     const uint32_t call = DROP ? a.rnd.call() : 0;
@@ -98,8 +98,8 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
         next_ok = (uint32_t)__ballot(px >= 0);
         if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
-        load_operand<T, D>(kk, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h, f.vec_k);
-        load_operand<T, D>(v, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h, f.vec_v);
+        load_operand<T, D, VEC>(kk, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h);
+        load_operand<T, D, VEC>(v, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h);
     };
     if (first < end) {
         fetch(k[0]);
@@ -310,11 +310,14 @@ static hipError_t run_split(FwdArgs& f, const Cut& c, hipStream_t st)
     const int items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
     f.items = items * f.shares;
     const int lds = std::max(4 * Tile<T, D>::BYTES, 4 * (D * 32 + 64) * (int)sizeof(float));
+    // (what is not in whole pieces takes the kernel with dropout, which drops nothing below a threshold of 0)
     static LdsOptIn opt;
-    hipError_t e = opt.ensure({(const void*)region_fwd_kernel<T, D, 1, true, true>, (const void*)region_fwd_kernel<T, D, 1, false, true>}, lds);
+    hipError_t e = opt.ensure({(const void*)region_fwd_kernel<T, D, 1, true, true, true>, (const void*)region_fwd_kernel<T, D, 1, false, true, true>,
+                               (const void*)region_fwd_kernel<T, D, 1, true, true, false>}, lds);
     if (e != hipSuccess) return e;
-    if (f.a.rnd.threshold) region_fwd_kernel<T, D, 1, true, true><<<f.items, 256, lds, st>>>(f);
-    else region_fwd_kernel<T, D, 1, false, true><<<f.items, 256, lds, st>>>(f);
+    const auto kernel = !f.vec ? region_fwd_kernel<T, D, 1, true, true, false>
+                      : f.a.rnd.threshold ? region_fwd_kernel<T, D, 1, true, true, true> : region_fwd_kernel<T, D, 1, false, true, true>;
+    kernel<<<f.items, 256, lds, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess || f.shares == 1) return e;
     region_fwd_join_kernel<T, D><<<dim3(items, (std::min(f.a.R, 32) + 3) / 4), 256, 0, st>>>(f);
     return hipGetLastError();
@@ -327,8 +330,9 @@ static hipError_t run(FwdArgs& f, hipStream_t st)
     const long long items = (long long)f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
     f.items = (int)items;
     const int blocks = (int)((items + 3) / 4), lds = 4 * Tile<T, D>::BYTES;
-    if (f.a.rnd.threshold) region_fwd_kernel<T, D, NR, true, false><<<blocks, 256, lds, st>>>(f);
-    else region_fwd_kernel<T, D, NR, false, false><<<blocks, 256, lds, st>>>(f);
+    const auto kernel = !f.vec ? region_fwd_kernel<T, D, 1, true, false, false>
+                      : f.a.rnd.threshold ? region_fwd_kernel<T, D, NR, true, false, true> : region_fwd_kernel<T, D, NR, false, false, true>;
+    kernel<<<blocks, 256, lds, st>>>(f);
     return hipGetLastError();
 }
 
@@ -336,14 +340,12 @@ template <typename T>
 static hipError_t run_t(FwdArgs& f, hipStream_t st)
 {
     const Args& a = f.a;
-    f.vec_q = pieces(a.q, a.qs, a.d, sizeof(T));
-    f.vec_k = pieces(a.k, a.ks, a.d, sizeof(T));
-    f.vec_v = pieces(a.v, a.vs, a.d, sizeof(T));
+    f.vec = pieces(a.q, a.qs, a.d, sizeof(T)) && pieces(a.k, a.ks, a.d, sizeof(T)) && pieces(a.v, a.vs, a.d, sizeof(T));
     f.vec_o = a.d % 4 == 0 && ((uintptr_t)f.out & (4 * sizeof(T) - 1)) == 0;
     const Cut c = cut(a);
     if (c.split) return a.d <= 32 ? run_split<T, 32>(f, c, st) : a.d <= 64 ? run_split<T, 64>(f, c, st) : run_split<T, 128>(f, c, st);
     // two row tiles per wave read every key operand half as often, where the registers hold them
-    const bool two = a.R > 32;
+    const bool two = a.R > 32 && f.vec;
     if (a.d <= 32) return two ? run<T, 32, 2>(f, st) : run<T, 32, 1>(f, st);
     if (a.d <= 64) return two && sizeof(T) == 2 ? run<T, 64, 2>(f, st) : run<T, 64, 1>(f, st);
     return run<T, 128, 1>(f, st);

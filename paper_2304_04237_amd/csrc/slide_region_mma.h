@@ -41,41 +41,50 @@ template <typename T, int D> __device__ __forceinline__ constexpr int piece_chan
     return sizeof(T) == 2 ? 16 * i + 8 * h : h * (D / 2) + 4 * i;
 }
 
-// One 16-byte piece of a pixel's channels, zeros beyond `left` channels.  vec: the pieces are whole and 16-byte aligned.
-__device__ __forceinline__ u4 load_piece(const bf16_bits* p, int left, bool vec)
+// One 16-byte piece of a pixel's channels, element by element, zeros beyond `left` channels
+__device__ __forceinline__ u4 gather_piece(const bf16_bits* p, int left)
 {
     u4 x = {0, 0, 0, 0};
-    if (vec) {
-        if (left > 0) x = *(const u4*)p;
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) x[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
-    }
+    for (int e = 0; e < 8; ++e)
+        if (e < left) x[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
     return x;
 }
-__device__ __forceinline__ f4 load_piece(const float* p, int left, bool vec)
+__device__ __forceinline__ f4 gather_piece(const float* p, int left)
 {
     f4 x = {0, 0, 0, 0};
-    if (vec) {
-        if (left > 0) x = *(const f4*)p;
-    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) x[e] = p[e];
-    }
+    for (int e = 0; e < 4; ++e)
+        if (e < left) x[e] = p[e];
     return x;
 }
 
-// The operand whose lane is one pixel's channels at p; zeros where the pixel does not count
-template <typename T, int D>
-__device__ __forceinline__ void load_operand(Operand<T, D>& o, const T* p, bool ok, int d, int h, bool vec)
+// The operand whose lane is one pixel's channels at p; zeros where the pixel does not count, and beyond its d channels.
+// VEC: the pieces are whole and 16-byte aligned; where, as mostly, nothing is to be left out, the loads follow each other without a test.
+template <typename T, int D, bool VEC>
+__device__ __forceinline__ void load_operand(Operand<T, D>& o, const T* p, bool ok, int d, int h)
 {
+    typedef decltype(gather_piece(p, 0)) Piece;
     constexpr int N = sizeof(T) == 2 ? D / 16 : D / 8;
+    if constexpr (VEC) {
+        if (d == D && __ballot(ok) == ~0ull) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = piece_channel<T, D>(i, h);
-        o.v[i] = load_piece(p + c, ok ? d - c : 0, vec);
+            for (int i = 0; i < N; ++i) o.v[i] = *(const Piece*)(p + piece_channel<T, D>(i, h));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) o.v[i] = Piece{0, 0, 0, 0};
+            if (ok) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (piece_channel<T, D>(i, h) < d) o.v[i] = *(const Piece*)(p + piece_channel<T, D>(i, h));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = piece_channel<T, D>(i, h);
+            o.v[i] = gather_piece(p + c, ok ? d - c : 0);
+        }
     }
 }
 
