@@ -64,7 +64,8 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int item = (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
     if (item >= f.items) return;
-    unsigned char* tile = lds + wave * Tile<T, D>::BYTES;
+    unsigned char* tile_k = lds + wave * 2 * Tile<T, D>::BYTES;
+    unsigned char* tile_v = tile_k + Tile<T, D>::BYTES;
     const int group = item / f.tiles, row0 = (item - group * f.tiles) * 32 * NR;
     const int bm = group / a.qm.regions, i = group - bm * a.qm.regions;
     const int b = bm / a.kv, m = bm - b * a.kv;
@@ -113,23 +114,23 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
-    Operand<T, D> kn, vn;
+    Rows<T, D> kn, vn;
     int region = walk.look(a, col, f.slots);
     uint32_t next_word = 0, next_ok;
     auto fetch = [&]() {
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
         next_ok = (uint32_t)__ballot(px >= 0);
         if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
-        load_operand<T, D, VEC>(kn, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h);
-        load_operand<T, D, VEC>(vn, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h);
+        kn.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.d, lane);
+        vn.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.d, lane);
     };
     fetch();
     region = walk.look(a, 32 + col, f.slots);
     for (int x = 0; x < f.slots; x += 32) {
-        const Operand<T, D> k = kn, v = vn;
         const uint32_t ok = next_ok, word = next_word;
         wave_order();
-        stage<D>(tile, k, lane);
+        kn.stage(tile_k, lane);
+        vn.stage(tile_v, lane);
         wave_order();
         if (x + 32 < f.slots) {
             fetch();
@@ -144,6 +145,9 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
                 quad[u] = h ? hi : lo;
             }
         }
+        Operand<T, D> k, v;
+        read_operand<D>(k, tile_k, lane);
+        read_operand<D>(v, tile_v, lane);
         Weights<T> w[NA];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
             w[n].set(ds);
             if (FIX) w[NR + n].set(s);
         }
-        accumulate<D, NA>(acc, tile, w, lane);
+        accumulate<D, NA>(acc, tile_k, w, lane);
     }
 
 #pragma unroll
@@ -351,8 +355,10 @@ __global__ __launch_bounds__(64 * TEAM) void region_dkdv_kernel(BwdArgs f)
     int qh, qw;
     a.qm.limits(b, qh, qw);
     const long long n_px = (long long)a.qm.H * a.qm.W;
-    Operand<T, D> q, g;
+    Rows<T, D> q, g;
     float st;
+    const T* qp = (const T*)a.q + b * a.qs.image;
+    const T* gp = (const T*)f.dout + b * n_px * a.heads * a.d;
     // step s: row tile s % row_tiles of the group of entry from + s / row_tiles
     const int steps = (to - from) * f.row_tiles;
     auto group_of = [&](int s) { return s < steps ? sorted[from + f.by_row_tiles.of(s)].x : 0; };
@@ -360,9 +366,8 @@ __global__ __launch_bounds__(64 * TEAM) void region_dkdv_kernel(BwdArgs f)
         const int r = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32 + col;
         const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
         const int px = r < a.R ? a.qm.pixel(i, place, qh, qw) : -1;
-        const bool ok = px >= 0;
-        load_operand<T, D, VEC>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h);
-        load_operand<T, D, VEC>(g, (const T*)f.dout + (ok ? ((long long)b * n_px + px) * a.heads * a.d + head * a.d : 0), ok, a.d, h);
+        q.template load<VEC>(qp, row_offset<VEC, T>(px, a.qs.pixel, head * a.d), a.d, lane);
+        g.template load<VEC>(gp, row_offset<VEC, T>(px, (long long)a.heads * a.d, head * a.d), a.d, lane);
         st = (h ? f.row_D : f.row_lse)[((long long)bm * a.qm.regions + i) * f.row_tiles * 32 + r];
     };
     int next = group_of(0), i = next;
@@ -371,17 +376,19 @@ __global__ __launch_bounds__(64 * TEAM) void region_dkdv_kernel(BwdArgs f)
     for (int s = 0; s < steps; ++s) {
         const int r0 = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32;
         wave_order();
-        stage<D>(tile_q, q, lane);
-        stage<D>(tile_g, g, lane);
+        q.stage(tile_q, lane);
+        g.stage(tile_g, lane);
         stat[lane] = st;
         wave_order();
-        const Operand<T, D> qc = q, gc = g;
         const uint32_t pair0 = (uint32_t)i * a.pairs + (r0 >> 1);
         if (s + 1 < steps) {
             fetch(s + 1, next);
             i = next;
             next = group_of(s + 2);
         }
+        Operand<T, D> qc, gc;
+        read_operand<D>(qc, tile_q, lane);
+        read_operand<D>(gc, tile_g, lane);
         float lse[16], Dr[16];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -562,7 +569,11 @@ static hipError_t run_rows(BwdArgs& f, hipStream_t st)
 {
     f.tiles = (f.a.R + 32 * NR - 1) / (32 * NR);
     f.items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
-    const int blocks = (f.items + 3) / 4, lds = 4 * Tile<T, D>::BYTES;
+    const int blocks = (f.items + 3) / 4, lds = 8 * Tile<T, D>::BYTES;
+    static LdsOptIn opt;
+    const hipError_t e = opt.ensure({(const void*)region_dq_kernel<T, D, 1, true, false>, (const void*)region_dq_kernel<T, D, NR, true, true>,
+                                     (const void*)region_dq_kernel<T, D, NR, false, true>}, lds);
+    if (e != hipSuccess) return e;
     // (what is not in whole pieces takes the kernels with dropout, which drop nothing below a threshold of 0)
     const auto kernel = !f.vec ? region_dq_kernel<T, D, 1, true, false>
                       : f.a.rnd.threshold ? region_dq_kernel<T, D, NR, true, true> : region_dq_kernel<T, D, NR, false, true>;
@@ -598,8 +609,9 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
 {
     const Args& a = f.a;
     const Strides whole{(long long)a.heads * a.d, (long long)a.qm.H * a.qm.W * a.heads * a.d};
-    f.vec = pieces(a.q, a.qs, a.d, sizeof(T)) && pieces(a.k, a.ks, a.d, sizeof(T)) && pieces(a.v, a.vs, a.d, sizeof(T)) &&
-            pieces(f.dout, whole, a.d, sizeof(T)) && pieces(f.out, whole, a.d, sizeof(T));
+    const long long nq = (long long)a.qm.H * a.qm.W, nk = (long long)a.km.H * a.km.W;
+    f.vec = pieces(a.q, a.qs, a.d, sizeof(T), nq) && pieces(a.k, a.ks, a.d, sizeof(T), nk) && pieces(a.v, a.vs, a.d, sizeof(T), nk) &&
+            pieces(f.dout, whole, a.d, sizeof(T), nq) && pieces(f.out, whole, a.d, sizeof(T), nq);
     plan<T>(f);
     const Room r = room<T>(f);
     f.row_lse = (float*)(ws + r.lse); f.row_D = (float*)(ws + r.D); f.sorted = (int2*)(ws + r.sorted);

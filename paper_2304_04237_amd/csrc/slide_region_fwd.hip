@@ -3,7 +3,7 @@
 // One wave takes 32 NR rows of a group and walks over the group's keys, the slots of the listed regions one after the other, 32 at
 // a time: S^T = K Q^T (keys are rows of the result, so a lane holds 16 keys of one query row and the softmax needs one exchange
 // between the lane halves), P = exp2(S c - m) with a running maximum m and sum, O^T += V^T P^T.  P stays in the registers in which the
-// first product leaves it.  K goes from memory into operands, V through 32 rows of LDS that only this wave uses; both are loaded
+// first product leaves it.  K and V come by way of 32 rows of LDS each that only this wave uses, loaded
 // one tile ahead.  Waves share nothing, so no barrier is passed and the waves of a compute unit cover each other's latencies.
 //
 // Few rows over many keys (one new token) leave most of the chip idle that way.  Then the keys of a group are split: the four waves
@@ -43,7 +43,8 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
     const int work = SPLIT ? (int)xcd_order(blockIdx.x, gridDim.x) : (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
     if (work >= f.items) return;
     const int item = SPLIT ? work / f.shares : work, share = SPLIT ? work - item * f.shares : 0;
-    unsigned char* tile = lds + wave * Tile<T, D>::BYTES;
+    unsigned char* tile_k = lds + wave * 2 * Tile<T, D>::BYTES;
+    unsigned char* tile_v = tile_k + Tile<T, D>::BYTES;
     int first = 0, end = f.slots;
     if (SPLIT) {
         const int key_tiles = (f.slots + 31) / 32, parts = 4 * f.shares, w = 4 * share + wave;
@@ -90,32 +91,33 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
-    Operand<T, D> k[2], v;
+    Rows<T, D> k, v;
     int region = walk.look(a, first + col, end);
     uint32_t word, next_word = 0;
     uint32_t ok, next_ok;
-    auto fetch = [&](Operand<T, D>& kk) {
+    auto fetch = [&]() {
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
         next_ok = (uint32_t)__ballot(px >= 0);
         if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
-        load_operand<T, D, VEC>(kk, kp + (px < 0 ? 0 : px) * a.ks.pixel, px >= 0, a.d, h);
-        load_operand<T, D, VEC>(v, vp + (px < 0 ? 0 : px) * a.vs.pixel, px >= 0, a.d, h);
+        k.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.d, lane);
+        v.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.d, lane);
     };
     if (first < end) {
-        fetch(k[0]);
+        fetch();
         region = walk.look(a, first + 32 + col, end);
     }
 
-    auto step = [&](const Operand<T, D>& kk, Operand<T, D>& kn, int x) {
+    for (int x = first; x < end; x += 32) {
         ok = next_ok; word = next_word;
         wave_order();
-        stage<D>(tile, v, lane);
+        k.stage(tile_k, lane);
+        v.stage(tile_v, lane);
         wave_order();
         if (x + 32 < end) {
-            fetch(kn);
+            fetch();
             region = walk.look(a, x + 64 + col, end);
         }
-        if (ok == 0) return;
+        if (ok == 0) continue;
         uint32_t quad[4];
         if (DROP) {
 #pragma unroll
@@ -124,6 +126,8 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
                 quad[u] = h ? hi : lo;
             }
         }
+        Operand<T, D> kk;
+        read_operand<D>(kk, tile_k, lane);
         Weights<T> w[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -161,11 +165,7 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
             }
             w[n].set(s);
         }
-        accumulate<D, NR>(o, tile, w, lane);
-    };
-    for (int x = first; x < end; x += 64) {
-        step(k[0], k[1], x);
-        if (x + 32 < end) step(k[1], k[0], x + 32);
+        accumulate<D, NR>(o, tile_v, w, lane);
     }
 
     if constexpr (SPLIT) {
@@ -309,7 +309,7 @@ static hipError_t run_split(FwdArgs& f, const Cut& c, hipStream_t st)
     f.shares = c.shares;
     const int items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
     f.items = items * f.shares;
-    const int lds = std::max(4 * Tile<T, D>::BYTES, 4 * (D * 32 + 64) * (int)sizeof(float));
+    const int lds = std::max(8 * Tile<T, D>::BYTES, 4 * (D * 32 + 64) * (int)sizeof(float));
     // (what is not in whole pieces takes the kernel with dropout, which drops nothing below a threshold of 0)
     static LdsOptIn opt;
     hipError_t e = opt.ensure({(const void*)region_fwd_kernel<T, D, 1, true, true, true>, (const void*)region_fwd_kernel<T, D, 1, false, true, true>,
@@ -329,7 +329,11 @@ static hipError_t run(FwdArgs& f, hipStream_t st)
     f.tiles = (f.a.R + 32 * NR - 1) / (32 * NR);
     const long long items = (long long)f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
     f.items = (int)items;
-    const int blocks = (int)((items + 3) / 4), lds = 4 * Tile<T, D>::BYTES;
+    const int blocks = (int)((items + 3) / 4), lds = 8 * Tile<T, D>::BYTES;
+    static LdsOptIn opt;
+    const hipError_t e = opt.ensure({(const void*)region_fwd_kernel<T, D, NR, true, false, true>, (const void*)region_fwd_kernel<T, D, NR, false, false, true>,
+                                     (const void*)region_fwd_kernel<T, D, 1, true, false, false>}, lds);
+    if (e != hipSuccess) return e;
     const auto kernel = !f.vec ? region_fwd_kernel<T, D, 1, true, false, false>
                       : f.a.rnd.threshold ? region_fwd_kernel<T, D, NR, true, false, true> : region_fwd_kernel<T, D, NR, false, false, true>;
     kernel<<<blocks, 256, lds, st>>>(f);
@@ -340,7 +344,8 @@ template <typename T>
 static hipError_t run_t(FwdArgs& f, hipStream_t st)
 {
     const Args& a = f.a;
-    f.vec = pieces(a.q, a.qs, a.d, sizeof(T)) && pieces(a.k, a.ks, a.d, sizeof(T)) && pieces(a.v, a.vs, a.d, sizeof(T));
+    const long long nq = (long long)a.qm.H * a.qm.W, nk = (long long)a.km.H * a.km.W;
+    f.vec = pieces(a.q, a.qs, a.d, sizeof(T), nq) && pieces(a.k, a.ks, a.d, sizeof(T), nk) && pieces(a.v, a.vs, a.d, sizeof(T), nk);
     f.vec_o = a.d % 4 == 0 && ((uintptr_t)f.out & (4 * sizeof(T) - 1)) == 0;
     const Cut c = cut(a);
     if (c.split) return a.d <= 32 ? run_split<T, 32>(f, c, st) : a.d <= 64 ? run_split<T, 64>(f, c, st) : run_split<T, 128>(f, c, st);
