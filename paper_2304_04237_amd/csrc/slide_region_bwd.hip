@@ -129,13 +129,11 @@ __global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
     for (int x = 0; x < f.slots; x += 32) {
         const uint32_t ok = next_ok, word = next_word;
         wave_order();
-        kn.stage(tile_k, lane);
-        vn.stage(tile_v, lane);
+        kn.stage(tile_k, ok, a.d, lane);
+        vn.stage(tile_v, ok, a.d, lane);
         wave_order();
-        if (x + 32 < f.slots) {
-            fetch();
-            region = walk.look(a, x + 64 + col, f.slots);
-        }
+        fetch();
+        region = walk.look(a, x + 64 + col, f.slots);
         if (ok == 0) continue;
         uint32_t quad[4];
         if (DROP) {
@@ -357,35 +355,38 @@ __global__ __launch_bounds__(64 * TEAM) void region_dkdv_kernel(BwdArgs f)
     const long long n_px = (long long)a.qm.H * a.qm.W;
     Rows<T, D> q, g;
     float st;
+    uint32_t next_ok = 0;
     const T* qp = (const T*)a.q + b * a.qs.image;
     const T* gp = (const T*)f.dout + b * n_px * a.heads * a.d;
     // step s: row tile s % row_tiles of the group of entry from + s / row_tiles
     const int steps = (to - from) * f.row_tiles;
-    auto group_of = [&](int s) { return s < steps ? sorted[from + f.by_row_tiles.of(s)].x : 0; };
+    auto group_of = [&](int s) { return sorted[from + f.by_row_tiles.of(min(s, steps - 1))].x; };
     auto fetch = [&](int s, int i) {
         const int r = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32 + col;
         const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
-        const int px = r < a.R ? a.qm.pixel(i, place, qh, qw) : -1;
+        const int there = a.qm.pixel(i, r < a.R ? place : 0, qh, qw), px = r < a.R ? there : -1;
+        next_ok = (uint32_t)__ballot(px >= 0);
         q.template load<VEC>(qp, row_offset<VEC, T>(px, a.qs.pixel, head * a.d), a.d, lane);
         g.template load<VEC>(gp, row_offset<VEC, T>(px, (long long)a.heads * a.d, head * a.d), a.d, lane);
         st = (h ? f.row_D : f.row_lse)[((long long)bm * a.qm.regions + i) * f.row_tiles * 32 + r];
     };
-    int next = group_of(0), i = next;
-    if (steps > 0) fetch(0, next);
-    next = group_of(1);
+    int next = 0, i = 0;
+    if (steps > 0) {
+        i = group_of(0);
+        fetch(0, i);
+        next = group_of(1);
+    }
     for (int s = 0; s < steps; ++s) {
         const int r0 = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32;
         wave_order();
-        q.stage(tile_q, lane);
-        g.stage(tile_g, lane);
+        q.stage(tile_q, next_ok, a.d, lane);
+        g.stage(tile_g, next_ok, a.d, lane);
         stat[lane] = st;
         wave_order();
         const uint32_t pair0 = (uint32_t)i * a.pairs + (r0 >> 1);
-        if (s + 1 < steps) {
-            fetch(s + 1, next);
-            i = next;
-            next = group_of(s + 2);
-        }
+        fetch(min(s + 1, steps - 1), next);         // (the last step's again, behind the end)
+        i = next;
+        next = group_of(s + 2);
         Operand<T, D> qc, gc;
         read_operand<D>(qc, tile_q, lane);
         read_operand<D>(gc, tile_g, lane);

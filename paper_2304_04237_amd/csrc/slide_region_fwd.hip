@@ -102,21 +102,16 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         k.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.d, lane);
         v.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.d, lane);
     };
-    if (first < end) {
-        fetch();
-        region = walk.look(a, first + 32 + col, end);
-    }
-
+    fetch();
+    region = walk.look(a, first + 32 + col, end);
     for (int x = first; x < end; x += 32) {
         ok = next_ok; word = next_word;
         wave_order();
-        k.stage(tile_k, lane);
-        v.stage(tile_v, lane);
+        k.stage(tile_k, ok, a.d, lane);
+        v.stage(tile_v, ok, a.d, lane);
         wave_order();
-        if (x + 32 < end) {
-            fetch();
-            region = walk.look(a, x + 64 + col, end);
-        }
+        fetch();
+        region = walk.look(a, x + 64 + col, end);
         if (ok == 0) continue;
         uint32_t quad[4];
         if (DROP) {

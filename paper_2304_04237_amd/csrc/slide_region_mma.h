@@ -119,21 +119,23 @@ template <typename T, int D> struct Tile {
     static __device__ __forceinline__ int at(int row, int c) { return row * D * (int)sizeof(T) + ((c ^ exchange(row)) << 4); }
 };
 
-// Where a row of a tile begins: in 16-byte pieces if the tensor is made of whole pieces (VEC), else in elements; all ones: nowhere, zeros.
+// Where a row of a tile begins: in 16-byte pieces if the tensor is made of whole pieces (VEC), else in elements
 template <bool VEC> struct Offset { typedef uint32_t type; };
 template <> struct Offset<false> { typedef long long type; };
 
+// ... of pixel px; of pixel 0 for a row that does not count (which is read all the same, and left out on its way to the tile)
 template <bool VEC, typename T>
 __device__ __forceinline__ typename Offset<VEC>::type row_offset(int px, long long pixel_stride, int channel)
 {
-    if constexpr (VEC) return px < 0 ? ~0u : (uint32_t)px * (uint32_t)(pixel_stride * (int)sizeof(T) >> 4) + (uint32_t)(channel * (int)sizeof(T) >> 4);
-    else return px < 0 ? -1 : px * pixel_stride + channel;
+    if constexpr (VEC) return (uint32_t)max(px, 0) * (uint32_t)(pixel_stride * (int)sizeof(T) >> 4) + (uint32_t)(channel * (int)sizeof(T) >> 4);
+    else return max(px, 0) * pixel_stride + channel;
 }
 
 // 32 rows of D channels on their way from memory to a tile.  Consecutive lanes take consecutive pieces of a row: a load in which every lane
-// has a row of its own takes the vector cache four times as long (59 against 16 accesses; the whole dq kernel 146 against 75 us without).
+// has a row of its own takes the vector cache four times as long (59 against 16 accesses; 16384 tokens: dq 146 against 118 us).
+// Loading makes no decision, so that it can be scheduled into the products; what does not count is set to zero by stage().
 template <typename T, int D> struct Rows {
-    static constexpr int PER_ROW = D * (int)sizeof(T) / 16, N = 32 * PER_ROW / 64;
+    static constexpr int PER_ROW = D * (int)sizeof(T) / 16, N = 32 * PER_ROW / 64, E = 16 / (int)sizeof(T);
     typedef typename std::conditional<sizeof(T) == 2, u4, f4>::type Piece;
     Piece v[N];
 
@@ -142,31 +144,25 @@ template <typename T, int D> struct Rows {
     __device__ __forceinline__ void load(const T* base, typename Offset<VEC>::type at, int d, int lane)
     {
         const int c = lane % PER_ROW;
-        if constexpr (VEC) {
-            uint32_t off[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) off[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((64 * i + lane) / PER_ROW), (int)at);
-            if (d == D && __ballot(at == ~0u) == 0) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = ((const Piece*)base)[(uint64_t)off[i] + c];
+        for (int i = 0; i < N; ++i) {
+            if constexpr (VEC) {
+                const uint32_t off = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((64 * i + lane) / PER_ROW), (int)at);
+                v[i] = ((const Piece*)base)[(uint64_t)off + (c * E < d ? c : 0)];
             } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = Piece{0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (off[i] != ~0u && c * (int)(16 / sizeof(T)) < d) v[i] = ((const Piece*)base)[(uint64_t)off[i] + c];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
                 const long long off = __shfl(at, (64 * i + lane) / PER_ROW);
-                const int channel = c * (int)(16 / sizeof(T));
-                v[i] = gather_piece(base + (off < 0 ? 0 : off) + channel, off < 0 ? 0 : d - channel);
+                v[i] = gather_piece(base + off + c * E, d - c * E);
             }
         }
     }
-    __device__ __forceinline__ void stage(unsigned char* tile, int lane) const
+    // ok: the rows that count, one bit each
+    __device__ __forceinline__ void stage(unsigned char* tile, uint32_t ok, int d, int lane)
     {
+        if (ok != 0xffffffffu || d != D) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (!(ok >> ((64 * i + lane) / PER_ROW) & 1) || lane % PER_ROW * E >= d) v[i] = Piece{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) *(Piece*)(tile + Tile<T, D>::at((64 * i + lane) / PER_ROW, lane % PER_ROW)) = v[i];
     }
@@ -292,12 +288,15 @@ struct Walk {
     {
         entry = a.by_slots.of(x);
         place = x - entry * 4 * a.quads;
-        return x < end ? list[entry] : -1;
+        const int j = list[min(entry, a.T - 1)];
+        return x < end ? j : -1;
     }
     // pixel of (region j, place), -1 if there is none
     static __device__ __forceinline__ int pixel(const Args& a, int j, int place, int vh, int vw)
     {
-        return j >= 0 && j < a.km.regions && place < a.km.places ? a.km.pixel(j, place, vh, vw) : -1;
+        const bool listed = (uint32_t)j < (uint32_t)a.km.regions && place < a.km.places;
+        const int px = a.km.pixel(listed ? j : 0, listed ? place : 0, vh, vw);
+        return listed ? px : -1;
     }
 };
 
