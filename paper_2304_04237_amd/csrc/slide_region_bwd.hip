@@ -56,7 +56,7 @@ template <> __device__ __forceinline__ float piece_dot<float>(const u4& a, const
 // bf16: out was rounded, so dout.out is off by up to 2^-8 of its terms.  The sum of P F dP, which is D without that, is only known at
 // the end; until then the rounded D0 is used, and dq is corrected by (D - D0) sum P k, for one more product.
 template <typename T, int D, int NR, bool DROP, bool VEC>
-__global__ __launch_bounds__(256) void region_dq_kernel(BwdArgs f)
+__global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
 {
     constexpr bool FIX = sizeof(T) == 2;
     const Args& a = f.a;
@@ -279,34 +279,36 @@ __device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint3
 
 // dk and dv of 32 NK keys of a region, by one wave or a team of four that divide the entries among them and add their sums in LDS.
 template <typename T, int D, int NK, bool DROP, int TEAM, bool VEC>
-__global__ __launch_bounds__(64 * TEAM) void region_dkdv_kernel(BwdArgs f)
+__global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
 {
     const Args& a = f.a;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = TEAM == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int item = (int)xcd_order(blockIdx.x, gridDim.x);
     unsigned char* tile_q = lds + wave * (2 * Tile<T, D>::BYTES + 256);
     unsigned char* tile_g = tile_q + Tile<T, D>::BYTES;
     float* stat = (float*)(tile_g + Tile<T, D>::BYTES);        // lse, then D, of 32 rows
     const int J = a.km.regions, col = lane & 31, h = lane >> 5;
 
-    // this block's work: the first `share` entries of a region (units 0 .. J - 1), or those of a window that lie beyond (the rest)
-    const int per_image = (J + f.windows) * f.key_tiles;
-    const int bm = item / per_image;
-    int unit = item - bm * per_image;
+    // this block's work: the first `share` entries of a region, or, behind all of those, the entries of a window that lie beyond.
+    // (Each part is spread over the XCDs: there is little to do in the second.)
+    const int firsts = a.B * a.kv * J * f.key_tiles;
+    const bool beyond = (int)blockIdx.x >= firsts;
+    int unit = beyond ? (int)xcd_order(blockIdx.x - firsts, gridDim.x - firsts) : (int)xcd_order(blockIdx.x, firsts);
     const int kt = unit % f.key_tiles;
     unit /= f.key_tiles;
+    const int units = beyond ? f.windows : J, bm = unit / units;
+    unit -= bm * units;
     const int b = bm / a.kv, m = bm - b * a.kv;
     const int* start = f.start + (long long)bm * (J + 1);
     const int2* sorted = f.sorted + (long long)bm * f.entries;
     int j = unit, from, to, slot = -1;
-    if (unit < J) {
+    if (!beyond) {
         from = start[j];
         const int end = start[j + 1];
         to = min(end, from + f.share);
         if (end > to) slot = 2 * (from / f.share);
     } else {
-        const int window = unit - J;
+        const int window = unit;
         if ((long long)window * f.share >= start[J]) return;
         j = sorted[window * f.share].y;
         from = max(window * f.share, start[j] + f.share);
