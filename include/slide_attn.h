@@ -394,7 +394,7 @@ int slide_region_attn_bwd(const slide_region_problem* p, const void* dout, const
  * keep(i) is 65536 / (65536 - t), t = p rounded to 65536ths, where half word i % 8 of Philox-4x32-7 with key seed and counter
  * (low 32 bits of i / 8, high 32 bits of i / 8 with the top bit set, 2^32 - 1, offset) is at least t, and 0 elsewhere (a dropped
  * element contributes nothing, whatever it holds).  p, seed, offset, offset_device as for the attention weights of
- * slide_region_problem; the two draw from disjoint counters.  The mask is never stored.  1 <= n < 2^48.
+ * slide_region_problem; the two draw from disjoint counters.  The mask is never stored.  1 <= n < 2^34.
  */
 int slide_dropout_fwd(const void* x, const void* residual, void* y, long long n, int dtype, float p,
                       unsigned long long seed, unsigned int offset, const long long* offset_device, void* stream);

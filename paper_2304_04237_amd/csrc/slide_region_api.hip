@@ -145,7 +145,7 @@ static int dropout(const void* x, const void* residual, void* y, long long n, in
 {
     if (dtype != SLIDE_F32 && dtype != SLIDE_BF16) return SLIDE_ERR_DTYPE;
     slide::region::Random r;
-    if (n < 1 || n >= 1ll << 48 || !make_random(p, seed, offset, offset_device, r)) return SLIDE_ERR_SHAPE;
+    if (n < 1 || n >= 1ll << 34 || !make_random(p, seed, offset, offset_device, r)) return SLIDE_ERR_SHAPE;
     if (!x || !y) return SLIDE_ERR_NULL;
     const size_t esz = dtype == SLIDE_F32 ? 4 : 2;
     if (!aligned(x, esz) || !aligned(residual, esz) || !aligned(y, esz) || !aligned(offset_device, 8)) return SLIDE_ERR_ALIGN;

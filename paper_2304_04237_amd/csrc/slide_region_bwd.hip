@@ -1,8 +1,8 @@
 // Region attention, backward, on the matrix cores.
 //
 //   P = exp(S - lse);  D = dout.out;  dS = P (F dP - D),  dP = dout.v,  F the weights' dropout factors
-//   dq = scale sum dS k   (row kernel: a wave per 32 NR rows of a group, over the group's keys, like the forward)
-//   dk = scale sum dS q,  dv = sum F P dout   (key kernel: a wave per 32 NK keys of a region, over the rows of the groups that list it)
+//   dq = scale sum dS k   (row kernel: a wave per 32 rows of a group, over the group's keys, like the forward)
+//   dk = scale sum dS q,  dv = sum F P dout   (key kernel: a wave per 32 keys of a region, over the rows of the groups that list it)
 //
 // Between the two a kernel turns the lists around (which groups list region j, in ascending order, so that sums have one order).
 // A block takes at most `share` of a region's groups; what is beyond goes to further blocks, whose float32 sums a last kernel adds up.
@@ -23,8 +23,8 @@ struct BwdArgs {
     float* row_D;
     int2* sorted;           // [B * kv][regions of q * T]: (group, region) of every entry that counts, by region, then by group
     int* start;             // [B * kv][J + 1]
-    float* partial;         // [B * kv][key tiles][2 windows][2][32 NK][D]
-    int slots, tiles, row_tiles, key_tiles, items;
+    float* partial;         // [B * kv][key tiles][2 windows][2][32][D]
+    int slots, row_tiles, key_tiles, items;
     int entries;            // regions of q * T
     int share, windows;     // entries per block of the key kernel, ceil(entries / share)
     int team;               // waves that share a tile of keys, 1 or 4
@@ -55,7 +55,7 @@ template <> __device__ __forceinline__ float piece_dot<float>(const u4& a, const
 // dq and, for the key kernel, every row's lse and D.
 // bf16: out was rounded, so dout.out is off by up to 2^-8 of its terms.  The sum of P F dP, which is D without that, is only known at
 // the end; until then the rounded D0 is used, and dq is corrected by (D - D0) sum P k, for one more product.
-template <typename T, int D, int NR, bool DROP, bool VEC>
+template <typename T, int D, bool DROP, bool VEC>
 __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
 {
     constexpr bool FIX = sizeof(T) == 2;
@@ -66,43 +66,41 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
     if (item >= f.items) return;
     unsigned char* tile_k = lds + wave * 2 * Tile<T, D>::BYTES;
     unsigned char* tile_v = tile_k + Tile<T, D>::BYTES;
-    const int group = item / f.tiles, row0 = (item - group * f.tiles) * 32 * NR;
+    const int group = item / f.row_tiles, row0 = (item - group * f.row_tiles) * 32;
     const int bm = group / a.qm.regions, i = group - bm * a.qm.regions;
     const int b = bm / a.kv, m = bm - b * a.kv;
-    const int col = lane & 31, h = lane >> 5;
+    const int col = lane & 31, h = lane >> 5, r = row0 + col;
 
-    Operand<T, D> q[NR], g[NR];
-    long long out_at[NR];
-    float row_lse[NR], D0[NR], D1[NR];
+    // this lane's row.  With dropout dP is used without the factor 1 / keep of the weights that are kept, and D divided by it:
+    // keep (dP - D / keep); what is summed of it is multiplied at the end
+    const float keep = DROP ? a.rnd.scale : 1.0f;
+    Operand<T, D> q, g;
+    long long out_at;
+    float row_lse, D0, D1 = 0.0f;
     {
         int vh, vw;
         a.qm.limits(b, vh, vw);
+        const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
+        const int px = r < a.R ? a.qm.pixel(i, place, a.qm.H, a.qm.W) : -1;
+        const bool ok = r < a.R && a.qm.pixel(i, place, vh, vw) >= 0;
+        const long long n_px = (long long)a.qm.H * a.qm.W;
+        out_at = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
+        const long long at = ok ? out_at : 0;
+        load_operand<T, D, VEC>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h);
+        load_operand<T, D, VEC>(g, (const T*)f.dout + at, ok, a.d, h);
+        Operand<T, D> o;
+        load_operand<T, D, VEC>(o, (const T*)f.out + at, ok, a.d, h);
+        float s = 0.0f;
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            const int r = row0 + 32 * n + col;
-            const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
-            const int px = r < a.R ? a.qm.pixel(i, place, a.qm.H, a.qm.W) : -1;
-            const bool ok = r < a.R && a.qm.pixel(i, place, vh, vw) >= 0;
-            const long long n_px = (long long)a.qm.H * a.qm.W;
-            out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
-            const long long at = ok ? out_at[n] : 0;
-            load_operand<T, D, VEC>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h);
-            load_operand<T, D, VEC>(g[n], (const T*)f.dout + at, ok, a.d, h);
-            Operand<T, D> o;
-            load_operand<T, D, VEC>(o, (const T*)f.out + at, ok, a.d, h);
-            float s = 0.0f;
-#pragma unroll
-            for (int u = 0; u < (int)(sizeof(o) / 16); ++u)
-                s += piece_dot<T>(__builtin_bit_cast(u4, o.v[u]), __builtin_bit_cast(u4, g[n].v[u]));
-            D0[n] = halves_sum(s);
-            D1[n] = 0.0f;
-            const float l = ok ? f.lse[((long long)b * a.heads + head) * n_px + px] : -INFINITY;
-            row_lse[n] = l == -INFINITY ? INFINITY : l * LOG2E;
-        }
+        for (int u = 0; u < (int)(sizeof(o) / 16); ++u)
+            s += piece_dot<T>(__builtin_bit_cast(u4, o.v[u]), __builtin_bit_cast(u4, g.v[u]));
+        D0 = halves_sum(s) / keep;
+        const float l = ok ? f.lse[((long long)b * a.heads + head) * n_px + px] : -INFINITY;
+        row_lse = l == -INFINITY ? INFINITY : l * LOG2E;
     }
     const uint32_t call = DROP ? a.rnd.call() : 0;
-    const float c2 = a.scale * LOG2E, keep = DROP ? a.rnd.scale : 1.0f;
-    constexpr int NA = FIX ? 2 * NR : NR;
+    const float c2 = a.scale * LOG2E;
+    constexpr int NA = FIX ? 2 : 1;
     f16v acc[NA][D / 32];           // sums of dS k, then of P k
 #pragma unroll
     for (int n = 0; n < NA; ++n)
@@ -135,73 +133,59 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         fetch();
         region = walk.look(a, x + 64 + col, f.slots);
         if (ok == 0) continue;
-        uint32_t quad[4];
-        if (DROP) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t lo = __builtin_amdgcn_readlane(word, 8 * u), hi = __builtin_amdgcn_readlane(word, 8 * u + 4);
-                quad[u] = h ? hi : lo;
-            }
-        }
         Operand<T, D> k, v;
         read_operand<D>(k, tile_k, lane);
         read_operand<D>(v, tile_v, lane);
-        Weights<T> w[NA];
+        f16v s = dot<D>(k, q, f16v{});
+        f16v p = dot<D>(v, g, f16v{});              // dP
+        if (ok != 0xffffffffu) {
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            f16v s = dot<D>(k, q[n], f16v{});
-            f16v p = dot<D>(v, g[n], f16v{});           // dP
-            if (ok != 0xffffffffu) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!((ok >> acc_row(r, 0)) >> (4 * h) & 1)) s[r] = -INFINITY;
-            }
-            if (DROP) {
-                uint32_t words[4][2];
-                row_keep(a.rnd, call, quad, (uint32_t)i * a.pairs + ((row0 + 32 * n + col) >> 1), bm, words);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    p[r] = (words[r >> 2][(r & 3) >> 1] >> (16 * (r & 1)) & 0xffffu) < a.rnd.threshold ? 0.0f : p[r] * keep;
-            }
-            f16v ds;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -row_lse[n]));
-                if (FIX) D1[n] = __builtin_fmaf(s[r], p[r], D1[n]);
-                ds[r] = s[r] * (p[r] - D0[n]);
-            }
-            w[n].set(ds);
-            if (FIX) w[NR + n].set(s);
+            for (int r = 0; r < 16; ++r)
+                if (!((ok >> acc_row(r, 0)) >> (4 * h) & 1)) s[r] = -INFINITY;
         }
+        if (DROP) {
+            uint32_t words[4][2];
+            row_keep(a.rnd, call, word, (uint32_t)i * a.pairs + (r >> 1), bm, words);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                p[r] = (words[r >> 2][(r & 3) >> 1] >> (16 * (r & 1)) & 0xffffu) < a.rnd.threshold ? 0.0f : p[r];
+        }
+        f16v ds;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -row_lse));
+            if (FIX) D1 = __builtin_fmaf(s[r], p[r], D1);
+            ds[r] = s[r] * (p[r] - D0);
+        }
+        Weights<T> w[NA];
+        w[0].set(ds);
+        if (FIX) w[NA - 1].set(s);
         accumulate<D, NA>(acc, tile_k, w, lane);
     }
 
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        const float exact = FIX ? halves_sum(D1[n]) : D0[n], fix = FIX ? exact - D0[n] : 0.0f;
-        const int r = row0 + 32 * n + col;
-        if (h == 0 && r < f.row_tiles * 32) {
-            const long long at = (long long)group * f.row_tiles * 32 + r;
-            f.row_lse[at] = row_lse[n];
-            f.row_D[at] = exact;
-        }
-        if (out_at[n] < 0) continue;
-        const bool valid = row_lse[n] != INFINITY;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int u = 0; u < 16; u += 4) {
-                const int c = 32 * dt + acc_row(u, h);
-                float x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = acc[n][dt][u + e];
-                    if (FIX) x[e] = __builtin_fmaf(-fix, acc[NA - NR + n][dt][u + e], x[e]);
-                    x[e] = valid ? x[e] * a.scale : 0.0f;
-                }
-                store4((T*)f.dq + out_at[n] + c, x, a.d - c, f.vec_dq);
-            }
+    const float exact = FIX ? halves_sum(D1) : D0, fix = exact - D0;
+    if (h == 0) {
+        const long long at = (long long)group * f.row_tiles * 32 + r;
+        f.row_lse[at] = row_lse;
+        f.row_D[at] = exact;
     }
+    if (out_at < 0) return;
+    const bool valid = row_lse != INFINITY;
+    const float up = a.scale * keep;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 16; u += 4) {
+            const int c = 32 * dt + acc_row(u, h);
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = acc[0][dt][u + e];
+                if (FIX) x[e] = __builtin_fmaf(-fix, acc[NA - 1][dt][u + e], x[e]);
+                x[e] = valid ? x[e] * up : 0.0f;
+            }
+            store4((T*)f.dq + out_at + c, x, a.d - c, f.vec_dq);
+        }
 }
 
 // The lists turned around: a wave per region of keys (or four, each over a quarter, where the lists are long) goes over
@@ -277,8 +261,8 @@ __device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint3
     pairs(std::integral_constant<int, 2>{}); pairs(std::integral_constant<int, 3>{});
 }
 
-// dk and dv of 32 NK keys of a region, by one wave or a team of four that divide the entries among them and add their sums in LDS.
-template <typename T, int D, int NK, bool DROP, int TEAM, bool VEC>
+// dk and dv of 32 keys of a region, by one wave or a team of four that divide the entries among them and add their sums in LDS.
+template <typename T, int D, bool DROP, int TEAM, bool VEC>
 __global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
 {
     const Args& a = f.a;
@@ -324,33 +308,27 @@ __global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
         from += mine;
     }
 
-    Operand<T, D> k[NK], v[NK];
-    long long out_at[NK];
-    bool valid[NK];
-    uint32_t quad[NK];
+    Operand<T, D> k, v;
+    long long out_at;
+    bool valid;
+    uint32_t quad;
     {
         int vh, vw;
         a.km.limits(b, vh, vw);
-#pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            const int place = (kt * NK + n) * 32 + col;
-            const int px = place < a.km.places ? a.km.pixel(j, place, a.km.H, a.km.W) : -1;
-            valid[n] = place < a.km.places && a.km.pixel(j, place, vh, vw) >= 0;
-            const long long n_px = (long long)a.km.H * a.km.W;
-            out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.kv * a.d + m * a.d;
-            quad[n] = (uint32_t)j * a.quads + (place >> 2);
-            const long long at = valid[n] ? px : 0;
-            load_operand<T, D, VEC>(k[n], (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.d, valid[n], a.d, h);
-            load_operand<T, D, VEC>(v[n], (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.d, valid[n], a.d, h);
-        }
+        const int place = kt * 32 + col;
+        const int px = place < a.km.places ? a.km.pixel(j, place, a.km.H, a.km.W) : -1;
+        valid = place < a.km.places && a.km.pixel(j, place, vh, vw) >= 0;
+        out_at = px < 0 ? -1 : ((long long)b * a.km.H * a.km.W + px) * a.kv * a.d + m * a.d;
+        quad = (uint32_t)j * a.quads + (place >> 2);
+        const long long at = valid ? px : 0;
+        load_operand<T, D, VEC>(k, (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.d, valid, a.d, h);
+        load_operand<T, D, VEC>(v, (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.d, valid, a.d, h);
     }
     const uint32_t call = DROP ? a.rnd.call() : 0;
-    const float c2 = a.scale * LOG2E, keep = DROP ? a.rnd.scale : 1.0f;
-    f16v dk[NK][D / 32], dv[NK][D / 32];
+    const float c2 = a.scale * LOG2E, keep = DROP ? a.rnd.scale : 1.0f;         // (as in the row kernel, row_D is divided by it)
+    f16v dk[1][D / 32], dv[1][D / 32];
 #pragma unroll
-    for (int n = 0; n < NK; ++n)
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) { dk[n][dt] = f16v{}; dv[n][dt] = f16v{}; }
+    for (int dt = 0; dt < D / 32; ++dt) { dk[0][dt] = f16v{}; dv[0][dt] = f16v{}; }
 
     int qh, qw;
     a.qm.limits(b, qh, qw);
@@ -399,90 +377,85 @@ __global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
 #pragma unroll
             for (int e = 0; e < 4; ++e) { lse[4 * u + e] = x[e]; Dr[4 * u + e] = y[e]; }
         }
-        Weights<T> wk[NK], wv[NK];
+        f16v p = dot<D>(qc, k, f16v{});
+        f16v ds = dot<D>(gc, v, f16v{});            // dP
+        uint32_t words[8][2];
+        if (DROP) {
+            key_keep(a.rnd, call, quad, pair0, h, bm, words);
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            f16v p = dot<D>(qc, k[n], f16v{});
-            f16v ds = dot<D>(gc, v[n], f16v{});
-            uint32_t words[8][2];
-            if (DROP) key_keep(a.rnd, call, quad[n], pair0, h, bm, words);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c2, -lse[r]));
-                bool kept = true;
-                if (DROP) kept = (words[r >> 1][r & 1] >> (16 * (lane & 1)) & 0xffffu) >= a.rnd.threshold;
-                ds[r] = p[r] * ((kept ? (DROP ? ds[r] * keep : ds[r]) : 0.0f) - Dr[r]);
-                if (DROP && !kept) p[r] = 0.0f;
-            }
-            wv[n].set(p);
-            wk[n].set(ds);
+            for (int r = 0; r < 16; ++r)
+                ds[r] = (words[r >> 1][r & 1] >> (16 * (lane & 1)) & 0xffffu) < a.rnd.threshold ? 0.0f : ds[r];
         }
-        accumulate<D, NK>(dv, tile_g, wv, lane);
-        accumulate<D, NK>(dk, tile_q, wk, lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c2, -lse[r]));
+            ds[r] = p[r] * (ds[r] - Dr[r]);
+            if (DROP) p[r] = (words[r >> 1][r & 1] >> (16 * (lane & 1)) & 0xffffu) < a.rnd.threshold ? 0.0f : p[r];
+        }
+        Weights<T> wk[1], wv[1];
+        wv[0].set(p);
+        wk[0].set(ds);
+        accumulate<D, 1>(dv, tile_g, wv, lane);
+        accumulate<D, 1>(dk, tile_q, wk, lane);
     }
 
     if constexpr (TEAM > 1) {
         // waves 2 and 3 hand their sums to 0 and 1, then 1 to 0; a lane's registers stay its own
         static_assert(TEAM == 4, "two rounds");
         float* room = (float*)lds + lane;
-        constexpr int N = 2 * NK * (D / 32) * 16;
+        constexpr int N = 2 * (D / 32) * 16;
 #pragma unroll
         for (int half = 2; half > 0; half >>= 1) {
             __syncthreads();
             float* to_lds = room + (wave & (half - 1)) * N * 64;
             if (wave >= half && wave < 2 * half) {
 #pragma unroll
-                for (int n = 0; n < NK; ++n)
+                for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            to_lds[((n * (D / 32) + dt) * 32 + r) * 64] = dk[n][dt][r];
-                            to_lds[((n * (D / 32) + dt) * 32 + 16 + r) * 64] = dv[n][dt][r];
-                        }
+                    for (int r = 0; r < 16; ++r) {
+                        to_lds[(dt * 32 + r) * 64] = dk[0][dt][r];
+                        to_lds[(dt * 32 + 16 + r) * 64] = dv[0][dt][r];
+                    }
             }
             __syncthreads();
             if (wave < half) {
 #pragma unroll
-                for (int n = 0; n < NK; ++n)
+                for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            dk[n][dt][r] += to_lds[((n * (D / 32) + dt) * 32 + r) * 64];
-                            dv[n][dt][r] += to_lds[((n * (D / 32) + dt) * 32 + 16 + r) * 64];
-                        }
+                    for (int r = 0; r < 16; ++r) {
+                        dk[0][dt][r] += to_lds[(dt * 32 + r) * 64];
+                        dv[0][dt][r] += to_lds[(dt * 32 + 16 + r) * 64];
+                    }
             }
         }
         if (wave > 0) return;
     }
-    float* part = f.partial + (((long long)bm * f.key_tiles + kt) * 2 * f.windows + max(slot, 0)) * (2 * 32 * NK * D);
+    float* part = f.partial + (((long long)bm * f.key_tiles + kt) * 2 * f.windows + max(slot, 0)) * (2 * 32 * D);
+    const float up = a.scale * keep;
 #pragma unroll
-    for (int n = 0; n < NK; ++n)
+    for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
+        for (int u = 0; u < 16; u += 4) {
+            const int c = 32 * dt + acc_row(u, h);
+            float x[4], y[4];
 #pragma unroll
-            for (int u = 0; u < 16; u += 4) {
-                const int c = 32 * dt + acc_row(u, h);
-                float x[4], y[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = valid[n] ? dk[n][dt][u + e] * a.scale : 0.0f;
-                    y[e] = valid[n] ? dv[n][dt][u + e] * keep : 0.0f;
-                }
-                if (slot >= 0) {
-                    float* p = part + (32 * n + col) * D + c;
-                    *(f4*)p = f4{x[0], x[1], x[2], x[3]};
-                    *(f4*)(p + 32 * NK * D) = f4{y[0], y[1], y[2], y[3]};
-                } else if (out_at[n] >= 0) {
-                    store4((T*)f.dk + out_at[n] + c, x, a.d - c, f.vec_dk);
-                    store4((T*)f.dv + out_at[n] + c, y, a.d - c, f.vec_dk);
-                }
+            for (int e = 0; e < 4; ++e) {
+                x[e] = valid ? dk[0][dt][u + e] * up : 0.0f;
+                y[e] = valid ? dv[0][dt][u + e] * keep : 0.0f;
             }
+            if (slot >= 0) {
+                float* p = part + col * D + c;
+                *(f4*)p = f4{x[0], x[1], x[2], x[3]};
+                *(f4*)(p + 32 * D) = f4{y[0], y[1], y[2], y[3]};
+            } else if (out_at >= 0) {
+                store4((T*)f.dk + out_at + c, x, a.d - c, f.vec_dk);
+                store4((T*)f.dv + out_at + c, y, a.d - c, f.vec_dk);
+            }
+        }
 }
 
 // The regions that more than `share` groups list: adds up the float32 sums of their waves, in order.
-template <typename T, int D, int NK>
+template <typename T, int D>
 __global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
 {
     const Args& a = f.a;
@@ -495,12 +468,12 @@ __global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
     const int j = f.sorted[(long long)bm * f.entries + (window + 1) * f.share].y;
     const int s = start[j], e = start[j + 1];
     if (s / f.share != window || e - s <= f.share) return;
-    const float* part = f.partial + ((long long)bm * f.key_tiles + kt) * 2 * f.windows * (2 * 32 * NK * D);
+    const float* part = f.partial + ((long long)bm * f.key_tiles + kt) * 2 * f.windows * (2 * 32 * D);
     const int last = (e - 1) / f.share;
-    for (int u = threadIdx.x; u < 2 * 32 * NK * D / 4; u += 256) {
-        f4 sum = *(const f4*)(part + (long long)(2 * window) * (2 * 32 * NK * D) + 4 * u);
-        for (int w = (s + f.share) / f.share; w <= last; ++w) sum += *(const f4*)(part + (long long)(2 * w + 1) * (2 * 32 * NK * D) + 4 * u);
-        const int c = 4 * u % D, place = kt * 32 * NK + 4 * u / D % (32 * NK), side = 4 * u / D / (32 * NK);
+    for (int u = threadIdx.x; u < 2 * 32 * D / 4; u += 256) {
+        f4 sum = *(const f4*)(part + (long long)(2 * window) * (2 * 32 * D) + 4 * u);
+        for (int w = (s + f.share) / f.share; w <= last; ++w) sum += *(const f4*)(part + (long long)(2 * w + 1) * (2 * 32 * D) + 4 * u);
+        const int c = 4 * u % D, place = kt * 32 + 4 * u / D % 32, side = 4 * u / D / 32;
         const int px = place < a.km.places ? a.km.pixel(j, place, a.km.H, a.km.W) : -1;
         if (px < 0) continue;
         const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
@@ -508,20 +481,16 @@ __global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
     }
 }
 
-// Two row tiles (or tiles of keys) per wave halve the reads of the other side's operands, where the registers hold them: the
-// sums take 2 x 16 registers per tile and 32 channels.
-template <typename T> static bool two_tiles(const BwdArgs& f, int n) { return sizeof(T) == 2 && f.a.d <= 32 && n > 32 && f.vec; }
-
 static int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
 // sizes that the workspace and the launches share
-template <typename T> static void plan(BwdArgs& f)
+static void plan(BwdArgs& f)
 {
     const Args& a = f.a;
     f.slots = 4 * a.quads * a.T;
     f.row_tiles = (a.R + 31) / 32;
     f.by_row_tiles = Div::by(f.row_tiles);
-    f.key_tiles = (a.km.places + (two_tiles<T>(f, a.km.places) ? 63 : 31)) / (two_tiles<T>(f, a.km.places) ? 64 : 32);
+    f.key_tiles = (a.km.places + 31) / 32;
     f.entries = a.qm.regions * a.T;
     // Four waves per tile of keys where a region has 24 row tiles or more on average (16384 tokens, 128 row tiles per region: 155
     // against 218 us); with few, as at stage 1 (8), the joining costs more than the finer division gives.
@@ -536,72 +505,61 @@ template <typename T> static void plan(BwdArgs& f)
 
 struct Room { size_t lse, D, sorted, start, partial, end; };
 
-template <typename T> static Room room(const BwdArgs& f)
+static Room room(const BwdArgs& f)
 {
     const Args& a = f.a;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     const size_t bm = (size_t)a.B * a.kv, rows = bm * a.qm.regions * f.row_tiles * 32 * sizeof(float);
-    const int nk = two_tiles<T>(f, a.km.places) ? 2 : 1;
     Room r;
     r.lse = 0;
     r.D = up(rows);
     r.sorted = r.D + up(rows);
     r.start = r.sorted + up(bm * f.entries * sizeof(int2));
     r.partial = r.start + up(bm * (a.km.regions + 1) * sizeof(int));
-    r.end = r.partial + bm * f.key_tiles * 2 * f.windows * (2 * 32 * nk * padded(a.d)) * sizeof(float);
+    r.end = r.partial + bm * f.key_tiles * 2 * f.windows * (2 * 32 * padded(a.d)) * sizeof(float);
     return r;
 }
 
-template <typename T> static size_t bytes_t(const Args& a)
+size_t bwd_workspace_bytes(const Args& a)
 {
-    size_t most = 0;                        // (whether the inputs come in whole pieces is known at the call only)
-    for (int vec = 0; vec < 2; ++vec) {
-        BwdArgs f{};
-        f.a = a;
-        f.vec = vec;
-        plan<T>(f);
-        most = std::max(most, room<T>(f).end);
-    }
-    return most;
+    BwdArgs f{};
+    f.a = a;
+    plan(f);
+    return room(f).end;
 }
 
-size_t bwd_workspace_bytes(const Args& a) { return a.dtype == 0 ? bytes_t<float>(a) : bytes_t<bf16_bits>(a); }
-
-template <typename T, int D, int NR>
+template <typename T, int D>
 static hipError_t run_rows(BwdArgs& f, hipStream_t st)
 {
-    f.tiles = (f.a.R + 32 * NR - 1) / (32 * NR);
-    f.items = f.a.B * f.a.kv * f.a.qm.regions * f.tiles;
+    f.items = f.a.B * f.a.kv * f.a.qm.regions * f.row_tiles;
     const int blocks = (f.items + 3) / 4, lds = 8 * Tile<T, D>::BYTES;
     static LdsOptIn opt;
-    const hipError_t e = opt.ensure({(const void*)region_dq_kernel<T, D, 1, true, false>, (const void*)region_dq_kernel<T, D, NR, true, true>,
-                                     (const void*)region_dq_kernel<T, D, NR, false, true>}, lds);
+    const hipError_t e = opt.ensure({(const void*)region_dq_kernel<T, D, true, false>, (const void*)region_dq_kernel<T, D, true, true>,
+                                     (const void*)region_dq_kernel<T, D, false, true>}, lds);
     if (e != hipSuccess) return e;
     // (what is not in whole pieces takes the kernels with dropout, which drop nothing below a threshold of 0)
-    const auto kernel = !f.vec ? region_dq_kernel<T, D, 1, true, false>
-                      : f.a.rnd.threshold ? region_dq_kernel<T, D, NR, true, true> : region_dq_kernel<T, D, NR, false, true>;
+    const auto kernel = !f.vec ? region_dq_kernel<T, D, true, false> : f.a.rnd.threshold ? region_dq_kernel<T, D, true, true> : region_dq_kernel<T, D, false, true>;
     kernel<<<blocks, 256, lds, st>>>(f);
     return hipGetLastError();
 }
 
-template <typename T, int D, int NK>
+template <typename T, int D>
 static hipError_t run_keys(BwdArgs& f, hipStream_t st)
 {
     const long long items = (long long)f.a.B * f.a.kv * f.key_tiles * (f.a.km.regions + f.windows);
-    const int one = 2 * Tile<T, D>::BYTES + 256, lds = f.team == 1 ? one : std::max(4 * one, 2 * 2 * NK * D * 32 * 4);
+    const int one = 2 * Tile<T, D>::BYTES + 256, lds = f.team == 1 ? one : std::max(4 * one, 2 * 2 * D * 32 * 4);
     static LdsOptIn opt;
-    hipError_t e = opt.ensure({(const void*)region_dkdv_kernel<T, D, NK, true, 4, true>, (const void*)region_dkdv_kernel<T, D, NK, false, 4, true>,
-                               (const void*)region_dkdv_kernel<T, D, 1, true, 4, false>}, 4 * one);
+    hipError_t e = opt.ensure({(const void*)region_dkdv_kernel<T, D, true, 4, true>, (const void*)region_dkdv_kernel<T, D, false, 4, true>,
+                               (const void*)region_dkdv_kernel<T, D, true, 4, false>}, 4 * one);
     if (e != hipSuccess) return e;
     const bool team = f.team > 1;
-    const auto kernel = !f.vec ? (team ? region_dkdv_kernel<T, D, 1, true, 4, false> : region_dkdv_kernel<T, D, 1, true, 1, false>)
-                      : f.a.rnd.threshold ? (team ? region_dkdv_kernel<T, D, NK, true, 4, true> : region_dkdv_kernel<T, D, NK, true, 1, true>)
-                                          : (team ? region_dkdv_kernel<T, D, NK, false, 4, true> : region_dkdv_kernel<T, D, NK, false, 1, true>);
+    const auto kernel = !f.vec ? (team ? region_dkdv_kernel<T, D, true, 4, false> : region_dkdv_kernel<T, D, true, 1, false>)
+                      : f.a.rnd.threshold ? (team ? region_dkdv_kernel<T, D, true, 4, true> : region_dkdv_kernel<T, D, true, 1, true>)
+                                          : (team ? region_dkdv_kernel<T, D, false, 4, true> : region_dkdv_kernel<T, D, false, 1, true>);
     kernel<<<(int)items, 64 * f.team, lds, st>>>(f);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     if (f.entries > f.share) {
-        region_dkdv_join_kernel<T, D, NK><<<f.a.B * f.a.kv * f.key_tiles * f.windows, 256, 0, st>>>(f);
+        region_dkdv_join_kernel<T, D><<<f.a.B * f.a.kv * f.key_tiles * f.windows, 256, 0, st>>>(f);
         e = hipGetLastError();
     }
     return e;
@@ -615,22 +573,20 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
     const long long nq = (long long)a.qm.H * a.qm.W, nk = (long long)a.km.H * a.km.W;
     f.vec = pieces(a.q, a.qs, a.d, sizeof(T), nq) && pieces(a.k, a.ks, a.d, sizeof(T), nk) && pieces(a.v, a.vs, a.d, sizeof(T), nk) &&
             pieces(f.dout, whole, a.d, sizeof(T), nq) && pieces(f.out, whole, a.d, sizeof(T), nq);
-    plan<T>(f);
-    const Room r = room<T>(f);
+    plan(f);
+    const Room r = room(f);
     f.row_lse = (float*)(ws + r.lse); f.row_D = (float*)(ws + r.D); f.sorted = (int2*)(ws + r.sorted);
     f.start = (int*)(ws + r.start); f.partial = (float*)(ws + r.partial);
     const uintptr_t quad = 4 * sizeof(T) - 1;
     f.vec_dq = a.d % 4 == 0 && ((uintptr_t)f.dq & quad) == 0;
     f.vec_dk = a.d % 4 == 0 && ((uintptr_t)f.dk & quad) == 0 && ((uintptr_t)f.dv & quad) == 0;
     hipError_t e;
-    if (two_tiles<T>(f, a.R)) e = run_rows<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
-    else e = a.d <= 32 ? run_rows<T, 32, 1>(f, st) : a.d <= 64 ? run_rows<T, 64, 1>(f, st) : run_rows<T, 128, 1>(f, st);
+    e = a.d <= 32 ? run_rows<T, 32>(f, st) : a.d <= 64 ? run_rows<T, 64>(f, st) : run_rows<T, 128>(f, st);
     if (e != hipSuccess) return e;
     f.invert_waves = f.entries >= 2048 ? 4 : 1;         // (196 entries: 5.5 us by one, 8.3 by four; 16384: 109 by one, 18 by four)
     region_invert_kernel<<<(int)(((long long)a.B * a.kv * a.km.regions * f.invert_waves + 3) / 4), 256, 0, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (two_tiles<T>(f, a.km.places)) return run_keys<T, 32, sizeof(T) == 2 ? 2 : 1>(f, st);
-    return a.d <= 32 ? run_keys<T, 32, 1>(f, st) : a.d <= 64 ? run_keys<T, 64, 1>(f, st) : run_keys<T, 128, 1>(f, st);
+    return a.d <= 32 ? run_keys<T, 32>(f, st) : a.d <= 64 ? run_keys<T, 64>(f, st) : run_keys<T, 128>(f, st);
 }
 
 hipError_t launch_bwd(const Args& a, const void* dout, const void* out, const float* lse, void* dq, void* dk, void* dv,

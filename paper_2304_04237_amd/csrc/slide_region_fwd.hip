@@ -113,14 +113,6 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         fetch();
         region = walk.look(a, x + 64 + col, end);
         if (ok == 0) continue;
-        uint32_t quad[4];
-        if (DROP) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t lo = __builtin_amdgcn_readlane(word, 8 * u), hi = __builtin_amdgcn_readlane(word, 8 * u + 4);
-                quad[u] = h ? hi : lo;
-            }
-        }
         Operand<T, D> kk;
         read_operand<D>(kk, tile_k, lane);
         Weights<T> w[NR];
@@ -153,7 +145,7 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
             }
             if (DROP) {
                 uint32_t words[4][2];
-                row_keep(a.rnd, call, quad, (uint32_t)i * a.pairs + ((row0 + 32 * n + col) >> 1), bm, words);
+                row_keep(a.rnd, call, word, (uint32_t)i * a.pairs + ((row0 + 32 * n + col) >> 1), bm, words);
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if ((words[r >> 2][(r & 3) >> 1] >> (16 * (r & 1)) & 0xffffu) < a.rnd.threshold) s[r] = 0.0f;

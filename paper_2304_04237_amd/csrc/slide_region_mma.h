@@ -300,23 +300,28 @@ struct Walk {
     }
 };
 
-// Random bits of the attention weights of one row tile: this lane's row (its pair and parity) and its 16 keys, quad q of which has
-// counter word quad[q].  Two rows share an evaluation, so each lane of a pair makes half of them and passes on what the other needs.
-__device__ __forceinline__ void row_keep(const Random& rnd, uint32_t call, const uint32_t (&quad)[4], uint32_t pair, uint32_t bm, uint32_t (&words)[4][2])
+// Random bits of the attention weights of one row tile: this lane's row (its pair and parity) and its 16 keys.  word: the counter word of
+// the four keys that this lane's key (lane % 32) is one of.  Two rows share an evaluation, so each lane of a pair makes half of them and
+// passes on what the other needs.  words[u][e]: elements 4 u + 2 e and the next, in halves.
+__device__ __forceinline__ void row_keep(const Random& rnd, uint32_t call, uint32_t word, uint32_t pair, uint32_t bm, uint32_t (&words)[4][2])
 {
-    const bool odd = threadIdx.x & 1;
-    Words x[2];
+    const bool odd = threadIdx.x & 1, upper = threadIdx.x & 32;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) x[u] = philox(odd ? quad[2 + u] : quad[u], pair, bm, call, rnd.key0, rnd.key1);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+        // this lane's evaluation: keys 4 lane half + 8 u .. for an even lane, 16 further for an odd one
+        const uint32_t e0 = __builtin_amdgcn_readlane(word, 8 * u), e1 = __builtin_amdgcn_readlane(word, 8 * u + 4);
+        const uint32_t o0 = __builtin_amdgcn_readlane(word, 8 * u + 16), o1 = __builtin_amdgcn_readlane(word, 8 * u + 20);
+        const uint32_t even_quad = upper ? e1 : e0, odd_quad = upper ? o1 : o0;
+        const Words x = philox(odd ? odd_quad : even_quad, pair, bm, call, rnd.key0, rnd.key1);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint32_t mine = odd ? x[u].w[2 + e] : x[u].w[e], pass = odd ? x[u].w[e] : x[u].w[2 + e];
+            const uint32_t first = x.w[e], second = x.w[2 + e];             // the even row's words, the odd row's
+            const uint32_t mine = odd ? second : first, pass = odd ? first : second;
             const uint32_t got = __builtin_amdgcn_mov_dpp(pass, 0xB1, 0xf, 0xf, true);         // from lane ^ 1
             words[u][e] = odd ? got : mine;
             words[2 + u][e] = odd ? mine : got;
         }
+    }
 }
 
 // whether the pieces of a tensor's pixels are whole, 16-byte aligned, and counted within an image by 32 bits

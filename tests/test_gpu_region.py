@@ -253,18 +253,22 @@ def test_values_that_are_not_finite():
 
 def test_a_cache_of_more_than_32_bits():
     """Keys and values behind 2^32 elements, queries of one token."""
-    n, d = 1 << 25, 128
-    k = torch.empty((1, 1, n, d), dtype=torch.bfloat16, device="cuda")
+    across, d = 1 << 16, 128                    # nine rows of 2^22 pixels
+    k = torch.empty((1, 9, 64 * across, d), dtype=torch.bfloat16, device="cuda")
     v = torch.empty_like(k)
-    lists = [0, n // 64 // 2, n // 64 - 2, n // 64 - 1]
+    lists = [0, 4 * across + 5, 9 * across - 2, 9 * across - 1]
     gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def part(x, j):
+        return x[:, j // across:j // across + 1, 64 * (j % across):64 * (j % across) + 64]
+
     for j in lists:
         for x in (k, v):
-            x[:, :, 64 * j:64 * j + 64] = torch.randn((1, 1, 64, d), generator=gen, device="cuda").bfloat16()
+            part(x, j).copy_(torch.randn((1, 1, 64, d), generator=gen, device="cuda"))
     q = torch.randn((1, 1, 1, 8 * d), generator=gen, device="cuda").bfloat16()
     index = torch.tensor(lists, dtype=torch.int32, device="cuda").reshape(1, 1, 1, 4)
     out = sa.slide_region_attn_fwd(q, k, v, index, heads=8, kv_heads=1, q_region=(1, 1), k_region=(1, 64))
-    near = {m: torch.cat([x[:, :, 64 * j:64 * j + 64] for j in lists], 2) for m, x in (("k", k), ("v", v))}
+    near = {m: torch.cat([part(x, j) for j in lists], 2) for m, x in (("k", k), ("v", v))}
     ref = ro.attention(numpy_of(q), numpy_of(near["k"]), numpy_of(near["v"]), np.arange(4).reshape(1, 1, 1, 4),
                        dict(heads=8, kv_heads=1, q_region=(1, 1), k_region=(1, 64)))
     assert off(out, ref["out"]) <= NORM["bf16"]
