@@ -28,7 +28,7 @@ struct BwdArgs {
     int entries;            // regions of q * T
     int share, windows;     // entries per block of the key kernel, ceil(entries / share)
     int team;               // waves that share a tile of keys, 1 or 4
-    int invert_waves;       // waves per region in the inversion, 1 or 4
+    int invert_waves;       // waves per region in the inversion, 1 or 16
     Div by_row_tiles;
     int vec, vec_dq, vec_dk;        // inputs in whole 16-byte pieces; dq, dk and dv in whole quads
 };
@@ -188,15 +188,15 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         }
 }
 
-// The lists turned around: a wave per region of keys (or four, each over a quarter, where the lists are long) goes over
-// all entries of its image and head, first counting, then writing in order.
-__global__ __launch_bounds__(256) void region_invert_kernel(BwdArgs f)
+// The lists turned around: a wave per region of keys (or sixteen, each over its part, where the lists are long)
+// goes over all entries of its image and head, first counting, then writing in order.
+__global__ __launch_bounds__(1024) void region_invert_kernel(BwdArgs f)
 {
     const Args& a = f.a;
-    __shared__ int2 counts[4];
+    __shared__ int2 counts[16];
     const int lane = threadIdx.x & 63, J = a.km.regions;
     const int waves = f.invert_waves, wave = (threadIdx.x >> 6) & (waves - 1), base = (threadIdx.x >> 6) - wave;
-    const long long id = (long long)blockIdx.x * (4 / waves) + base / waves;
+    const long long id = waves == 1 ? (long long)blockIdx.x * 4 + base : blockIdx.x;
     const bool live = id < (long long)a.B * a.kv * J;
     const int bm = live ? (int)(id / J) : 0, j = live ? (int)(id - (long long)bm * J) : -1;
     const int* list = a.index + (long long)bm * f.entries;
@@ -583,8 +583,11 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
     hipError_t e;
     e = a.d <= 32 ? run_rows<T, 32>(f, st) : a.d <= 64 ? run_rows<T, 64>(f, st) : run_rows<T, 128>(f, st);
     if (e != hipSuccess) return e;
-    f.invert_waves = f.entries >= 2048 ? 4 : 1;         // (196 entries: 5.5 us by one, 8.3 by four; 16384: 109 by one, 18 by four)
-    region_invert_kernel<<<(int)(((long long)a.B * a.kv * a.km.regions * f.invert_waves + 3) / 4), 256, 0, st>>>(f);
+    // (196 entries: 5.5 us by one wave, 8.3 by four; 16384: 109 by one, 19 by four, 12 by sixteen)
+    f.invert_waves = f.entries >= 2048 ? 16 : 1;
+    const int regions = a.B * a.kv * a.km.regions;
+    if (f.invert_waves == 1) region_invert_kernel<<<(regions + 3) / 4, 256, 0, st>>>(f);
+    else region_invert_kernel<<<regions, 1024, 0, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return a.d <= 32 ? run_keys<T, 32>(f, st) : a.d <= 64 ? run_keys<T, 64>(f, st) : run_keys<T, 128>(f, st);
 }

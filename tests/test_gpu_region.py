@@ -30,12 +30,23 @@ CASES = {
     "512_rows_a_group": case((1, 64), (1, 256), heads=8, kv_heads=1, d=16, q_region=(1, 64), k_region=(1, 128), topk=2),
     "many_small_regions": case((1, 200), heads=2, d=32, q_region=(1, 10), k_region=(1, 3), topk=64),
     "everyone_lists_the_same": case((20, 20), B=2, heads=2, d=32, q_region=(2, 2), k_region=(5, 5), topk=2, lists="all"),
+    "600_lists": case((1, 600), heads=4, kv_heads=2, d=32, q_region=(1, 1), k_region=(1, 8), topk=4),
+    "600_lists_64_channels": case((1, 600), B=2, heads=4, kv_heads=1, d=64, q_region=(1, 1), k_region=(1, 40), topk=4, sized=True),
+    "600_lists_128_channels": case((1, 600), heads=2, kv_heads=1, d=128, q_region=(1, 1), k_region=(1, 100), topk=4),
+    "600_lists_of_few": case((1, 600), (1, 50), heads=40, kv_heads=1, d=20, q_region=(1, 1), k_region=(1, 10), topk=4),
+    "600_lists_odd": case((1, 600), heads=2, d=35, q_region=(1, 1), k_region=(1, 8), topk=4),
+    "large_groups_of_few": case((32, 40), (8, 8), heads=1, d=48, q_region=(16, 20), k_region=(4, 4), topk=3),
+    "64_channels": case((24, 24), B=2, heads=2, d=64, q_region=(8, 8), topk=3, sized=True),
+    "96_channels": case((16, 16), heads=2, d=96, q_region=(8, 8), topk=3),
     "scale": case((8, 8), d=32, q_region=(4, 4), topk=2, scale=0.7),
     "steep": case((8, 8), d=32, q_region=(4, 4), topk=2, scale=3.0),
     "dropped_ragged": case((13, 19), B=2, heads=3, d=24, q_region=(4, 5), sized=True, dropout=0.3),
     "dropped_odd": case((9, 9), heads=6, kv_heads=2, d=32, q_region=(3, 3), k_region=(3, 5), topk=4, dropout=0.5),
     "dropped_stage_like": case((24, 32), q_region=(8, 8), topk=4, dropout=0.1),
     "dropped_sequence": case((1, 100), heads=8, kv_heads=2, d=64, q_region=(1, 16), k_region=(1, 20), topk=4, dropout=0.2),
+    "dropped_600_lists": case((1, 600), heads=4, kv_heads=2, d=32, q_region=(1, 1), k_region=(1, 9), topk=4, dropout=0.2),
+    "dropped_64_channels": case((24, 24), heads=2, d=64, q_region=(8, 8), topk=3, dropout=0.3),
+    "dropped_128_channels": case((1, 130), heads=4, kv_heads=1, d=128, q_region=(1, 32), k_region=(1, 32), topk=3, dropout=0.3),
     "dropped_one_token": case((1, 1), (1, 300), B=2, heads=8, kv_heads=2, d=128, q_region=(1, 1), k_region=(1, 63), topk=3, dropout=0.2),
 }
 
@@ -164,7 +175,7 @@ def test_parts_of_wider_tensors(dtype):
         assert torch.equal(u, w)
 
 
-@pytest.mark.parametrize("name", ["ragged_24_channels", "one_token_many_keys", "everyone_lists_the_same", "dropped_sequence"])
+@pytest.mark.parametrize("name", ["ragged_24_channels", "one_token_many_keys", "everyone_lists_the_same", "600_lists_64_channels", "dropped_sequence"])
 def test_the_same_twice_and_on_another_stream(name):
     t, index, how = make(CASES[name], "bf16", seed=7)
     g, idx, gh = on_gpu(t, index, how)
