@@ -186,23 +186,33 @@ def _device(q, maps):
     return device
 
 
-def _enqueue(index, call):
-    """call(stream) with the device made current where it is not."""
-    if torch.cuda.current_device() == index:
-        return call(_stream(index))
-    with torch.cuda.device(index):
-        return call(_stream(index))
+def _on_device(call):
+    """A call that finds its first tensor's device current (switching there and back costs more than a small call)."""
+    name = call.__code__.co_varnames[0]
+
+    @functools.wraps(call)
+    def enqueue(*args, **kw):
+        first = args[0] if args else kw.get(name)
+        if not isinstance(first, torch.Tensor) or not first.is_cuda or first.device.index == torch.cuda.current_device():
+            return call(*args, **kw)                    # (what is not on a GPU is refused by the call itself)
+        with torch.cuda.device(first.device):
+            return call(*args, **kw)
+    return enqueue
+
+
+@_on_device
+def _region_workspace_bytes(q, k, code, topk, heads, q_region, k_region, kv_heads):
+    maps = (("k", k), ("v", k))
+    plan = _plan(q, maps, heads, q_region, k_region, kv_heads, topk)
+    return int(_library().slide_region_workspace_bytes(plan.problem(None, None, _device(q, maps)), code))
 
 
 def slide_region_workspace_bytes(call, q, k, topk, heads, q_region, k_region, kv_heads=None):
     """Bytes of scratch of slide_region_select ("select"), slide_region_attn_fwd ("fwd") or slide_region_attn_bwd ("bwd")."""
-    maps = (("k", k), ("v", k))
-    plan = _plan(q, maps, heads, q_region, k_region, kv_heads, topk)
-    p = plan.problem(None, None, _device(q, maps))
-    code = {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call]
-    return int(_enqueue(q.device.index, lambda stream: _library().slide_region_workspace_bytes(p, code)))
+    return _region_workspace_bytes(q, k, {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call], topk, heads, q_region, k_region, kv_heads)
 
 
+@_on_device
 def slide_region_select(q, k, topk, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None, index=None, workspace=None):
     """The lists: int32 [B, kv_heads, regions of q, topk], ascending, -1 behind the last.
 
@@ -212,15 +222,13 @@ def slide_region_select(q, k, topk, heads, q_region, k_region, kv_heads=None, q_
     plan = _plan(q, maps, heads, q_region, k_region, kv_heads, topk)
     device = _device(q, maps)
     p = plan.problem(q_size, k_size, device)
-
-    def call(stream):
-        lists = q.new_empty(plan.lists, dtype=torch.int32) if index is None else index
-        at = _like(lists, "index", plan.lists, torch.int32, device)
-        ws, size, keep = plan.scratch(p, _SELECT, workspace, q, device.index)
-        _check(lib.slide_region_select(p, q.data_ptr(), k.data_ptr(), at, ws, size, stream))
-        return lists
-
-    return _enqueue(device.index, call)
+    if index is None:
+        index = q.new_empty(plan.lists, dtype=torch.int32)
+    else:
+        _like(index, "index", plan.lists, torch.int32, device)
+    ws, size, keep = plan.scratch(p, _SELECT, workspace, q, device.index)
+    _check(lib.slide_region_select(p, q.data_ptr(), k.data_ptr(), index.data_ptr(), ws, size, _stream(device.index)))
+    return index
 
 
 def _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset):
@@ -239,6 +247,7 @@ def _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_si
     return plan, p, _like(index, "index", plan.lists, torch.int32, device)
 
 
+@_on_device
 def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None, scale=None,
                           dropout=0.0, seed=0, offset=0, out=None, lse=None, workspace=None):
     """out: every row of q over the keys of its region's list.  lse: optional float32 [B, heads, H, W] tensor that receives
@@ -248,63 +257,64 @@ def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=No
     lib = _library()
     plan, p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
     device = q.device
+    if out is None:
+        out = q.new_empty(q.shape)
+    else:
+        _like(out, "out", q.shape, q.dtype, device)
+    lse_at = None if lse is None else _like(lse, "lse", plan.lse, torch.float32, device)
+    ws, size, keep = plan.scratch(p, _FWD, workspace, q, device.index)
+    _check(lib.slide_region_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, out.data_ptr(), lse_at, ws, size,
+                                     _stream(device.index)))
+    return out
 
-    def call(stream):
-        result = q.new_empty(q.shape) if out is None else out
-        out_at = _like(result, "out", q.shape, q.dtype, device)
-        lse_at = None if lse is None else _like(lse, "lse", plan.lse, torch.float32, device)
-        ws, size, keep = plan.scratch(p, _FWD, workspace, q, device.index)
-        _check(lib.slide_region_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, out_at, lse_at, ws, size, stream))
-        return result
 
-    return _enqueue(device.index, call)
-
-
+@_on_device
 def slide_region_attn_bwd(dout, q, k, v, index, out, lse, heads, q_region, k_region, kv_heads=None, q_size=None, k_size=None,
                           scale=None, dropout=0.0, seed=0, offset=0, outputs=None, workspace=None):
     """Returns (dq, dk, dv), contiguous.  out, lse: the forward's results for the same arguments."""
     lib = _library()
     plan, p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
     device = q.device
-
-    def call(stream):
-        dq, dk, dv = (q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)) if outputs is None else outputs
-        at = [_like(t, name, like.shape, q.dtype, device)
-              for t, name, like in ((dout, "dout", q), (out, "out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
-        lse_at = _like(lse, "lse", plan.lse, torch.float32, device)
-        ws, size, keep = plan.scratch(p, _BWD, workspace, q, device.index)
-        _check(lib.slide_region_attn_bwd(p, at[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, at[1], lse_at, *at[2:], ws, size, stream))
-        return dq, dk, dv
-
-    return _enqueue(device.index, call)
+    dq, dk, dv = (q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)) if outputs is None else outputs
+    at = [_like(t, name, like.shape, q.dtype, device)
+          for t, name, like in ((dout, "dout", q), (out, "out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
+    lse_at = _like(lse, "lse", plan.lse, torch.float32, device)
+    ws, size, keep = plan.scratch(p, _BWD, workspace, q, device.index)
+    _check(lib.slide_region_attn_bwd(p, at[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, at[1], lse_at, *at[2:], ws, size,
+                                     _stream(device.index)))
+    return dq, dk, dv
 
 
 def _dropout(entry, x, name, residual, p, seed, offset, y):
+    """entry's call: x, residual (False: it takes none), y, ..."""
     if not x.is_cuda:
         raise SlideAttnError("%s must live on the GPU" % name)
     if not x.is_contiguous():
         raise SlideAttnError("%s must be contiguous" % name)
-    if x.dtype not in _CODES:
+    code = _CODES.get(x.dtype)
+    if code is None:
         raise SlideAttnError("%s must be float32 or bfloat16, got %s" % (name, x.dtype))
-    p, seed, number, holder = _random(p, seed, offset, x.device)
+    device = x.device
+    p, seed, number, holder = _random(p, seed, offset, device)
+    if y is None:
+        y = x.new_empty(x.shape)
+    else:
+        _like(y, "the result", x.shape, x.dtype, device)
+    at = (y.data_ptr(),)
+    if residual is not False:
+        at = (None if residual is None else _like(residual, "residual", x.shape, x.dtype, device),) + at
+    if x.numel():
+        _check(entry(x.data_ptr(), *at, x.numel(), code, p, seed, number, holder, _stream(device.index)))
+    return y
 
-    def call(stream):
-        result = x.new_empty(x.shape) if y is None else y
-        at = (_like(result, "the result", x.shape, x.dtype, x.device),)
-        if residual is not False:
-            at = (None if residual is None else _like(residual, "residual", x.shape, x.dtype, x.device),) + at
-        if x.numel():
-            _check(entry(x.data_ptr(), *at, x.numel(), _CODES[x.dtype], p, seed, number, holder, stream))
-        return result
 
-    return _enqueue(x.device.index, call)
-
-
+@_on_device
 def slide_dropout_fwd(x, p, seed, offset=0, residual=None, out=None):
     """residual + dropout(x) of any contiguous tensor; the mask follows from seed, offset and the element's number."""
     return _dropout(_library().slide_dropout_fwd, x, "x", residual, p, seed, offset, out)
 
 
+@_on_device
 def slide_dropout_bwd(dout, p, seed, offset=0, dx=None):
     """The gradient of x (the residual's is dout itself), with the mask of the forward's p, seed and offset."""
     return _dropout(_library().slide_dropout_bwd, dout, "dout", False, p, seed, offset, dx)
