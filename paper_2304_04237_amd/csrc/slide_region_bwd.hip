@@ -112,8 +112,9 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
+    const int slots = walk.length(a);
     Rows<T, D> kn, vn;
-    int region = walk.look(a, col, f.slots);
+    int region = walk.look(a, col, slots);
     uint32_t next_word = 0, next_ok;
     auto fetch = [&]() {
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
@@ -123,15 +124,15 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         vn.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.d, lane);
     };
     fetch();
-    region = walk.look(a, 32 + col, f.slots);
-    for (int x = 0; x < f.slots; x += 32) {
+    region = walk.look(a, 32 + col, slots);
+    for (int x = 0; x < slots; x += 32) {
         const uint32_t ok = next_ok, word = next_word;
         wave_order();
         kn.stage(tile_k, ok, a.d, lane);
         vn.stage(tile_v, ok, a.d, lane);
         wave_order();
         fetch();
-        region = walk.look(a, x + 64 + col, f.slots);
+        region = walk.look(a, x + 64 + col, slots);
         if (ok == 0) continue;
         Operand<T, D> k, v;
         read_operand<D>(k, tile_k, lane);

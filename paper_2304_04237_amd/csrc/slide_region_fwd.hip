@@ -3,8 +3,12 @@
 // One wave takes 32 NR rows of a group and walks over the group's keys, the slots of the listed regions one after the other, 32 at
 // a time: S^T = K Q^T (keys are rows of the result, so a lane holds 16 keys of one query row and the softmax needs one exchange
 // between the lane halves), P = exp2(S c - m) with a running maximum m and sum, O^T += V^T P^T.  P stays in the registers in which the
-// first product leaves it.  K and V come by way of 32 rows of LDS each that only this wave uses, loaded
-// one tile ahead.  Waves share nothing, so no barrier is passed and the waves of a compute unit cover each other's latencies.
+// first product leaves it.  K and V come by way of 32 rows of LDS each that only this wave uses, loaded one tile ahead.  Waves share
+// nothing, so no barrier is passed and the waves of a compute unit cover each other's latencies.
+//
+// What bounds it: heads of 32 in bf16 the vector work (an exponential, a multiply-add, an addition, half a maximum and half a conversion
+// per weight; 2 x 200 x 333, 16 regions of 8x8: 114 us, without the matrix instructions 109, without the loads 90); float32 the matrix
+// instructions and that work in turn (stage 2: 50 us, of which 28 without and 22 with the matrix cores idle).
 //
 // Few rows over many keys (one new token) leave most of the chip idle that way.  Then the keys of a group are split: the four waves
 // of a block take a quarter each of a share of the keys and join their sums in LDS, and where one block per 32 rows is still too
@@ -91,6 +95,7 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
+    end = min(end, walk.length(a));
     Rows<T, D> k, v;
     int region = walk.look(a, first + col, end);
     uint32_t word, next_word = 0;
@@ -265,8 +270,9 @@ __global__ __launch_bounds__(256) void region_fwd_join_kernel(FwdArgs f)
         f.lse[((long long)b * a.heads + head) * n_px + px] = up == 0.0f ? -INFINITY : ((most == -INFINITY ? 0.0f : most) + log2f(all)) * LN2;
 }
 
-// How a problem is cut.  A block per 32 rows and share of the keys (SPLIT) where a wave per 32 rows would not give every SIMD one;
-// then as many shares as give every SIMD one, of at least two key tiles each.
+// How a problem is cut.  A block per 32 rows and share of the keys (SPLIT) where a wave per 32 rows would not give every SIMD one (8 new
+// tokens, 32 heads of 128 over 4096 keys: 236 us by 32 waves, 28 split); then as many shares as give every SIMD one wave, of at
+// least two key tiles each.
 struct Cut { bool split; int tiles, shares; };
 
 static Cut cut(const Args& a)
@@ -336,7 +342,8 @@ static hipError_t run_t(FwdArgs& f, hipStream_t st)
     f.vec_o = a.d % 4 == 0 && ((uintptr_t)f.out & (4 * sizeof(T) - 1)) == 0;
     const Cut c = cut(a);
     if (c.split) return a.d <= 32 ? run_split<T, 32>(f, c, st) : a.d <= 64 ? run_split<T, 64>(f, c, st) : run_split<T, 128>(f, c, st);
-    // two row tiles per wave read every key operand half as often, where the registers hold them
+    // Two row tiles per wave load and stage every key half as often, where the registers hold them (bf16; one tile: 2 x 200 x 333
+    // pixels, heads of 32: 130 against 115 us; 16384 tokens, heads of 64: 95 against 72)
     const bool two = a.R > 32 && f.vec;
     if (a.d <= 32) return two ? run<T, 32, 2>(f, st) : run<T, 32, 1>(f, st);
     if (a.d <= 64) return two && sizeof(T) == 2 ? run<T, 64, 2>(f, st) : run<T, 64, 1>(f, st);

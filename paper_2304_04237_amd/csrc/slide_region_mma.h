@@ -291,6 +291,17 @@ struct Walk {
         const int j = list[min(entry, a.T - 1)];
         return x < end ? j : -1;
     }
+    // slots up to the last entry that is a region: a region of queries outside its image, or in sight of few regions, has a list that ends early
+    __device__ __forceinline__ int length(const Args& a) const
+    {
+        int last = 0;
+        for (int t0 = 0; t0 < a.T; t0 += 64) {
+            const int t = t0 + (threadIdx.x & 63), j = list[min(t, a.T - 1)];
+            const uint64_t regions = __ballot(t < a.T && (uint32_t)j < (uint32_t)a.km.regions);
+            if (regions) last = t0 + 64 - __builtin_clzll(regions);
+        }
+        return last * 4 * a.quads;
+    }
     // pixel of (region j, place), -1 if there is none
     static __device__ __forceinline__ int pixel(const Args& a, int j, int place, int vh, int vw)
     {

@@ -45,6 +45,10 @@ def make(c, dtype, seed, padding=True):
         index = rng.integers(0, J, (B, kv, G, c["topk"]))
         index = np.where(rng.random(index.shape) < 0.15, rng.choice([-1, J, J + 7, -2 ** 31, 2 ** 31 - 1], index.shape), index)
         index[-1, -1, -1] = -1          # a group without any
+    elif c["lists"] == "early":         # one to three regions, then nothing, in every second group nothing at all
+        index = np.full((B, kv, G, c["topk"]), -1)
+        index[:, :, ::2, :3] = rng.integers(0, J, index[:, :, ::2, :3].shape)
+        index[:, :, ::4, 2] = -1
     else:                               # every group lists the same few regions
         index = np.broadcast_to(np.arange(c["topk"]) % J, (B, kv, G, c["topk"]))
     return t, np.ascontiguousarray(index, dtype=np.int32), how

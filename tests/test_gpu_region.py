@@ -38,6 +38,10 @@ CASES = {
     "large_groups_of_few": case((32, 40), (8, 8), heads=1, d=48, q_region=(16, 20), k_region=(4, 4), topk=3),
     "64_channels": case((24, 24), B=2, heads=2, d=64, q_region=(8, 8), topk=3, sized=True),
     "96_channels": case((16, 16), heads=2, d=96, q_region=(8, 8), topk=3),
+    "1024_entries": case((1, 70), (1, 300), heads=2, d=32, q_region=(1, 35), k_region=(1, 2), topk=1024),
+    "list_ends_early": case((20, 20), B=2, heads=2, d=32, q_region=(5, 5), topk=70, lists="early"),
+    "one_token_128_channels_many_keys": case((1, 1), (1, 9000), B=2, heads=8, kv_heads=2, d=128, q_region=(1, 1), k_region=(1, 64), topk=60, sized=True),
+    "map_as_one_region": case((30, 31), heads=1, d=32, q_region=(99, 99), k_region=(99, 99), topk=1, lists="all"),
     "scale": case((8, 8), d=32, q_region=(4, 4), topk=2, scale=0.7),
     "steep": case((8, 8), d=32, q_region=(4, 4), topk=2, scale=3.0),
     "dropped_ragged": case((13, 19), B=2, heads=3, d=24, q_region=(4, 5), sized=True, dropout=0.3),
@@ -47,6 +51,7 @@ CASES = {
     "dropped_600_lists": case((1, 600), heads=4, kv_heads=2, d=32, q_region=(1, 1), k_region=(1, 9), topk=4, dropout=0.2),
     "dropped_64_channels": case((24, 24), heads=2, d=64, q_region=(8, 8), topk=3, dropout=0.3),
     "dropped_128_channels": case((1, 130), heads=4, kv_heads=1, d=128, q_region=(1, 32), k_region=(1, 32), topk=3, dropout=0.3),
+    "dropped_one_token_many_keys": case((1, 1), (1, 5000), B=2, heads=16, kv_heads=2, d=64, q_region=(1, 1), k_region=(1, 33), topk=90, dropout=0.3),
     "dropped_one_token": case((1, 1), (1, 300), B=2, heads=8, kv_heads=2, d=128, q_region=(1, 1), k_region=(1, 63), topk=3, dropout=0.2),
 }
 
@@ -107,7 +112,7 @@ def test_selection(name, dtype):
     t, _, how = make(c, dtype, seed=4)
     x = clean(t)
     g, _, gh = on_gpu(t, np.zeros(1, np.int32), how)
-    for topk in sorted({1, c["topk"], c["topk"] + 3}):
+    for topk in sorted({1, c["topk"], min(c["topk"] + 3, 1024)}):
         print(name, dtype, topk, flush=True)
         got = sa.slide_region_select(g["q"], g["k"], topk, **{n: v for n, v in gh.items() if n != "scale"})
         assert (got.cpu().numpy() == ro.select(x["q"], x["k"], topk, how)).all()
@@ -260,6 +265,28 @@ def test_values_that_are_not_finite():
         whole = torch.ones_like(o, dtype=torch.bool)
         whole[:16, 3] = whole[16:32, 7] = whole[32:48] = False
         assert o[whole].isfinite().all() and lse[0, 0, 0, 32:48].isnan().all() and lse[0, 0, 0, :32].isfinite().all()
+
+
+def test_two_calls_at_once():
+    """Two streams, two problems, in turns; each has its own workspace."""
+    work, want = [], []
+    for name, seed in (("one_token_many_keys", 20), ("600_lists", 21)):
+        t, index, how = make(CASES[name], "bf16", seed)
+        g, idx, gh = on_gpu(t, index, how)
+        out, lse = forward(g, idx, gh)
+        work.append((g, idx, gh))
+        want.append((out, lse, *backward(g, idx, gh, out, lse)))
+    streams = [torch.cuda.Stream() for _ in work]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for n, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                out, lse = forward(*work[n])
+                got[n].append((out, lse, *backward(*work[n], out, lse)))
+    torch.cuda.synchronize()
+    for n in range(2):
+        assert all(torch.equal(a, b) for one in got[n] for a, b in zip(one, want[n]))
 
 
 def test_a_cache_of_more_than_32_bits():
