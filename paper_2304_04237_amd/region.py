@@ -176,6 +176,11 @@ def _plan(q, maps, heads, q_region, k_region, kv_heads, topk):
                     tuple(q_region), tuple(k_region), kv_heads, topk)
 
 
+def _empty(t):
+    """A contiguous tensor of t's shape (empty_like takes two thirds of new_empty's time, but keeps other orders)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _device(q, maps):
     device = q.device
     if not q.is_cuda:
@@ -258,7 +263,7 @@ def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=No
     plan, p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
     device = q.device
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _empty(q)
     else:
         _like(out, "out", q.shape, q.dtype, device)
     lse_at = None if lse is None else _like(lse, "lse", plan.lse, torch.float32, device)
@@ -275,7 +280,7 @@ def slide_region_attn_bwd(dout, q, k, v, index, out, lse, heads, q_region, k_reg
     lib = _library()
     plan, p, lists = _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_size, scale, dropout, seed, offset)
     device = q.device
-    dq, dk, dv = (q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)) if outputs is None else outputs
+    dq, dk, dv = (_empty(q), _empty(k), _empty(v)) if outputs is None else outputs
     at = [_like(t, name, like.shape, q.dtype, device)
           for t, name, like in ((dout, "dout", q), (out, "out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
     lse_at = _like(lse, "lse", plan.lse, torch.float32, device)
@@ -297,7 +302,7 @@ def _dropout(entry, x, name, residual, p, seed, offset, y):
     device = x.device
     p, seed, number, holder = _random(p, seed, offset, device)
     if y is None:
-        y = x.new_empty(x.shape)
+        y = torch.empty_like(x)
     else:
         _like(y, "the result", x.shape, x.dtype, device)
     at = (y.data_ptr(),)
