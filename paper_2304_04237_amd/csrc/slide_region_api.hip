@@ -47,7 +47,7 @@ static int check(const slide_region_problem* p, int call, Args& a)
     if (!make_map(p->q_h, p->q_w, p->q_region_h, p->q_region_w, p->q_size, a.qm) ||
         !make_map(p->k_h, p->k_w, p->k_region_h, p->k_region_w, p->k_size, a.km)) return SLIDE_ERR_SHAPE;
     const long long rows = (long long)a.qm.places * a.g;
-    if (rows * a.qm.regions >= 1ll << 31) return SLIDE_ERR_SHAPE;       // (the dropout counter's second word)
+    if (rows * a.qm.regions >= 1ll << 30) return SLIDE_ERR_SHAPE;       // (the dropout counter's second word; rows of a share)
     a.R = (int)rows;
     a.quads = (a.km.places + 3) / 4; a.pairs = (a.R + 1) / 2;
     a.by_g = slide::region::Div::by(a.g); a.by_slots = slide::region::Div::by(4 * a.quads);

@@ -29,7 +29,7 @@ struct BwdArgs {
     int share, windows;     // entries per block of the key kernel, ceil(entries / share)
     int team;               // waves that share a tile of keys, 1 or 4
     int invert_waves;       // waves per region in the inversion, 1 or 16
-    Div by_row_tiles;
+    Div by_rows;            // 2 pairs: slots of a group in the key kernel
     int vec, vec_dq, vec_dk;        // inputs in whole 16-byte pieces; dq, dk and dv in whole quads
 };
 
@@ -237,15 +237,16 @@ __global__ __launch_bounds__(1024) void region_invert_kernel(BwdArgs f)
 }
 
 // Random bits seen from a key (lane) and 16 rows (registers): a patch of 4 keys and 2 rows is four lanes wide, so each of four lanes makes two
-// of their eight evaluations.  Returns for row pair p (registers 2 p, 2 p + 1) the two words that hold this lane's keys.
-__device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint32_t quad, uint32_t pair0, int h, uint32_t bm, uint32_t (&words)[8][2])
+// of their eight evaluations.  pair: the counter word of the pair that row lane % 32 is one of.
+// Returns for row pair p (registers 2 p, 2 p + 1) the two words that hold this lane's keys.
+__device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint32_t quad, uint32_t pair, int h, uint32_t bm, uint32_t (&words)[8][2])
 {
     const int k = threadIdx.x & 3;
     Words x[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const int p = 4 * u + k;                // rows acc_row(2 p, h) and the next
-        x[u] = philox(quad, pair0 + 4 * (p >> 1) + 2 * h + (p & 1), bm, call, rnd.key0, rnd.key1);
+        const int p = 4 * u + k, row = 8 * (p >> 1) + 4 * h + 2 * (p & 1);      // rows acc_row(2 p, h) and the next
+        x[u] = philox(quad, (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)pair), bm, call, rnd.key0, rnd.key1);
     }
     auto from = [&](auto lane4, uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp(v, decltype(lane4)::value * 0x55, 0xf, 0xf, true); };
     auto pairs = [&](auto lane4) {
@@ -264,7 +265,7 @@ __device__ __forceinline__ void key_keep(const Random& rnd, uint32_t call, uint3
 
 // dk and dv of 32 keys of a region, by one wave or a team of four that divide the entries among them and add their sums in LDS.
 template <typename T, int D, bool DROP, int TEAM, bool VEC>
-__global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
+__global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3 : 2) : 1) void region_dkdv_kernel(BwdArgs f)
 {
     const Args& a = f.a;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -339,35 +340,45 @@ __global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
     uint32_t next_ok = 0;
     const T* qp = (const T*)a.q + b * a.qs.image;
     const T* gp = (const T*)f.dout + b * n_px * a.heads * a.d;
-    // step s: row tile s % row_tiles of the group of entry from + s / row_tiles
-    const int steps = (to - from) * f.row_tiles;
-    auto group_of = [&](int s) { return sorted[from + f.by_row_tiles.of(min(s, steps - 1))].x; };
-    auto fetch = [&](int s, int i) {
-        const int r = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32 + col;
+    // The rows of the groups one after the other, each group's padded to whole pairs (a patch of the dropout counter): slot y is row
+    // y % (2 pairs) of the group of entry from + y / (2 pairs), and a tile holds rows of several groups.
+    const int entries = to - from, steps = (entries * (2 * a.pairs) + 31) / 32;
+    int row = 0;                                // this lane's row of the tile that is loaded next, its entry in bounds or not
+    bool there = false;
+    uint32_t next_pair = 0, pair;
+    auto look = [&](int s) {
+        const int y = 32 * s + col, e = f.by_rows.of(y);
+        row = y - e * (2 * a.pairs);
+        there = e < entries && row < a.R;
+        return sorted[from + min(e, entries - 1)].x;
+    };
+    const float* rows_of_image = (h ? f.row_D : f.row_lse) + (long long)bm * a.qm.regions * f.row_tiles * 32;
+    auto fetch = [&](int i) {
+        const int r = there ? row : 0;
         const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
-        const int there = a.qm.pixel(i, r < a.R ? place : 0, qh, qw), px = r < a.R ? there : -1;
+        const int at = a.qm.pixel(i, place, qh, qw), px = there ? at : -1;
         next_ok = (uint32_t)__ballot(px >= 0);
         q.template load<VEC>(qp, row_offset<VEC, T>(px, a.qs.pixel, head * a.d), a.d, lane);
         g.template load<VEC>(gp, row_offset<VEC, T>(px, (long long)a.heads * a.d, head * a.d), a.d, lane);
-        st = (h ? f.row_D : f.row_lse)[((long long)bm * a.qm.regions + i) * f.row_tiles * 32 + r];
+        const float x = rows_of_image[i * (f.row_tiles * 32) + r];
+        st = there ? x : h ? 0.0f : INFINITY;
+        if (DROP) next_pair = (uint32_t)i * a.pairs + (r >> 1);
     };
-    int next = 0, i = 0;
+    int next = 0;
     if (steps > 0) {
-        i = group_of(0);
-        fetch(0, i);
-        next = group_of(1);
+        next = look(0);
+        fetch(next);
+        next = look(1);
     }
     for (int s = 0; s < steps; ++s) {
-        const int r0 = (s - f.by_row_tiles.of(s) * f.row_tiles) * 32;
         wave_order();
         q.stage(tile_q, next_ok, a.d, lane);
         g.stage(tile_g, next_ok, a.d, lane);
         stat[lane] = st;
         wave_order();
-        const uint32_t pair0 = (uint32_t)i * a.pairs + (r0 >> 1);
-        fetch(min(s + 1, steps - 1), next);         // (the last step's again, behind the end)
-        i = next;
-        next = group_of(s + 2);
+        pair = next_pair;
+        fetch(next);                            // (zeros' worth of rows behind the end)
+        next = look(s + 2);
         Operand<T, D> qc, gc;
         read_operand<D>(qc, tile_q, lane);
         read_operand<D>(gc, tile_g, lane);
@@ -382,7 +393,7 @@ __global__ __launch_bounds__(64 * TEAM, 1) void region_dkdv_kernel(BwdArgs f)
         f16v ds = dot<D>(gc, v, f16v{});            // dP
         uint32_t words[8][2];
         if (DROP) {
-            key_keep(a.rnd, call, quad, pair0, h, bm, words);
+            key_keep(a.rnd, call, quad, pair, h, bm, words);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 ds[r] = (words[r >> 1][r & 1] >> (16 * (lane & 1)) & 0xffffu) < a.rnd.threshold ? 0.0f : ds[r];
@@ -490,17 +501,18 @@ static void plan(BwdArgs& f)
     const Args& a = f.a;
     f.slots = 4 * a.quads * a.T;
     f.row_tiles = (a.R + 31) / 32;
-    f.by_row_tiles = Div::by(f.row_tiles);
+    const long long slots = 2ll * a.pairs;
+    f.by_rows = Div::by((uint32_t)slots);
     f.key_tiles = (a.km.places + 31) / 32;
     f.entries = a.qm.regions * a.T;
     // Four waves per tile of keys where a region has 24 row tiles or more on average (16384 tokens, 128 row tiles per region: 155
     // against 218 us); with few, as at stage 1 (8), the joining costs more than the finer division gives.
     const long long average = ((long long)f.entries + a.km.regions - 1) / a.km.regions;
-    f.team = average * f.row_tiles >= 24 ? 4 : 1;
+    f.team = average * slots >= 24 * 32 ? 4 : 1;
     // A block's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip
     const long long all = (long long)a.B * a.kv * f.key_tiles * f.entries * f.team;
     const long long fill = std::max((long long)f.team, all / (16ll * device_cu_count()));
-    f.share = (int)std::min(std::max(2 * average, (8ll + f.row_tiles - 1) / f.row_tiles), fill);
+    f.share = (int)std::min({std::max(2 * average, (8 * 32 + slots - 1) / slots), fill, (1ll << 30) / slots});
     f.windows = (f.entries + f.share - 1) / f.share;
 }
 
