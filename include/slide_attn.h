@@ -359,7 +359,8 @@ typedef struct {
 typedef enum { SLIDE_REGION_SELECT = 0, SLIDE_REGION_FWD = 1, SLIDE_REGION_BWD = 2 } slide_region_call;
 
 /* Bytes of device scratch, 16-byte aligned, that the call (a slide_region_call) needs; 0 for invalid arguments or if it needs
- * none.  Launches nothing; reads the compute-unit count of the current device (256 if there is none). */
+ * none.  Where a head or a stride is no multiple of 16 bytes they include copies of q, k and v (dout and out) that are; tensors that
+ * are merely not 16-byte aligned take slower loads.  Launches nothing; reads the compute-unit count of the current device (256 if there is none). */
 size_t slide_region_workspace_bytes(const slide_region_problem* p, int call);
 
 /*

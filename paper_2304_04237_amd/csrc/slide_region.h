@@ -86,6 +86,8 @@ struct Args {
     Div by_g, by_slots;                 // slots: 4 * quads, what a listed region takes in a group's row of keys
     Map qm, km;
     Strides qs, ks, vs;
+    Strides os;                         // of dout and out (backward)
+    int hd, dl;                         // q, k, v, dout and out as they are loaded: elements between heads, channels (zeros behind d)
     float scale;
     Random rnd;
     const void* q; const void* k; const void* v;

@@ -69,6 +69,8 @@ static int check(const slide_region_problem* p, int call, Args& a)
     }
     if (!aligned(p->q_size, 4) || !aligned(p->k_size, 4)) return SLIDE_ERR_ALIGN;
     a.qs = {p->q_pixel, p->q_image}; a.ks = {p->k_pixel, p->k_image}; a.vs = {p->v_pixel, p->v_image};
+    a.os = {(long long)p->heads * p->head_dim, (long long)p->q_h * p->q_w * p->heads * p->head_dim};
+    a.hd = a.dl = a.d;
     a.scale = p->scale > 0.0f ? p->scale : 1.0f / sqrtf((float)p->head_dim);
     return SLIDE_OK;
 }

@@ -85,11 +85,11 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         const bool ok = r < a.R && a.qm.pixel(i, place, vh, vw) >= 0;
         const long long n_px = (long long)a.qm.H * a.qm.W;
         out_at = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
-        const long long at = ok ? out_at : 0;
-        load_operand<T, D, VEC>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.d : 0), ok, a.d, h);
-        load_operand<T, D, VEC>(g, (const T*)f.dout + at, ok, a.d, h);
+        const long long at = ok ? b * a.os.image + px * a.os.pixel + head * a.hd : 0;
+        load_operand<T, D, VEC>(q, (const T*)a.q + b * a.qs.image + (ok ? px * a.qs.pixel + head * a.hd : 0), ok, a.dl, h);
+        load_operand<T, D, VEC>(g, (const T*)f.dout + at, ok, a.dl, h);
         Operand<T, D> o;
-        load_operand<T, D, VEC>(o, (const T*)f.out + at, ok, a.d, h);
+        load_operand<T, D, VEC>(o, (const T*)f.out + at, ok, a.dl, h);
         float s = 0.0f;
 #pragma unroll
         for (int u = 0; u < (int)(sizeof(o) / 16); ++u)
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) acc[n][dt] = f16v{};
 
-    const T* kp = (const T*)a.k + b * a.ks.image + m * a.d;
-    const T* vp = (const T*)a.v + b * a.vs.image + m * a.d;
+    const T* kp = (const T*)a.k + b * a.ks.image + m * a.hd;
+    const T* vp = (const T*)a.v + b * a.vs.image + m * a.hd;
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
@@ -120,16 +120,16 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
         next_ok = (uint32_t)__ballot(px >= 0);
         if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
-        kn.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.d, lane);
-        vn.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.d, lane);
+        kn.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.dl, lane);
+        vn.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.dl, lane);
     };
     fetch();
     region = walk.look(a, 32 + col, slots);
     for (int x = 0; x < slots; x += 32) {
         const uint32_t ok = next_ok, word = next_word;
         wave_order();
-        kn.stage(tile_k, ok, a.d, lane);
-        vn.stage(tile_v, ok, a.d, lane);
+        kn.stage(tile_k, ok, a.dl, lane);
+        vn.stage(tile_v, ok, a.dl, lane);
         wave_order();
         fetch();
         region = walk.look(a, x + 64 + col, slots);
@@ -323,8 +323,8 @@ __global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3
         out_at = px < 0 ? -1 : ((long long)b * a.km.H * a.km.W + px) * a.kv * a.d + m * a.d;
         quad = (uint32_t)j * a.quads + (place >> 2);
         const long long at = valid ? px : 0;
-        load_operand<T, D, VEC>(k, (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.d, valid, a.d, h);
-        load_operand<T, D, VEC>(v, (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.d, valid, a.d, h);
+        load_operand<T, D, VEC>(k, (const T*)a.k + b * a.ks.image + at * a.ks.pixel + m * a.hd, valid, a.dl, h);
+        load_operand<T, D, VEC>(v, (const T*)a.v + b * a.vs.image + at * a.vs.pixel + m * a.hd, valid, a.dl, h);
     }
     const uint32_t call = DROP ? a.rnd.call() : 0;
     const float c2 = a.scale * LOG2E, keep = DROP ? a.rnd.scale : 1.0f;         // (as in the row kernel, row_D is divided by it)
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3
     float st;
     uint32_t next_ok = 0;
     const T* qp = (const T*)a.q + b * a.qs.image;
-    const T* gp = (const T*)f.dout + b * n_px * a.heads * a.d;
+    const T* gp = (const T*)f.dout + b * a.os.image;
     // The rows of the groups one after the other, each group's padded to whole pairs (a patch of the dropout counter): slot y is row
     // y % (2 pairs) of the group of entry from + y / (2 pairs), and a tile holds rows of several groups.
     const int entries = to - from, steps = (entries * (2 * a.pairs) + 31) / 32;
@@ -358,8 +358,8 @@ __global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3
         const int place = a.by_g.of(r), head = m * a.g + r - place * a.g;
         const int at = a.qm.pixel(i, place, qh, qw), px = there ? at : -1;
         next_ok = (uint32_t)__ballot(px >= 0);
-        q.template load<VEC>(qp, row_offset<VEC, T>(px, a.qs.pixel, head * a.d), a.d, lane);
-        g.template load<VEC>(gp, row_offset<VEC, T>(px, (long long)a.heads * a.d, head * a.d), a.d, lane);
+        q.template load<VEC>(qp, row_offset<VEC, T>(px, a.qs.pixel, head * a.hd), a.dl, lane);
+        g.template load<VEC>(gp, row_offset<VEC, T>(px, a.os.pixel, head * a.hd), a.dl, lane);
         const float x = rows_of_image[i * (f.row_tiles * 32) + r];
         st = there ? x : h ? 0.0f : INFINITY;
         if (DROP) next_pair = (uint32_t)i * a.pairs + (r >> 1);
@@ -372,8 +372,8 @@ __global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3
     }
     for (int s = 0; s < steps; ++s) {
         wave_order();
-        q.stage(tile_q, next_ok, a.d, lane);
-        g.stage(tile_g, next_ok, a.d, lane);
+        q.stage(tile_q, next_ok, a.dl, lane);
+        g.stage(tile_g, next_ok, a.dl, lane);
         stat[lane] = st;
         wave_order();
         pair = next_pair;
@@ -538,7 +538,7 @@ size_t bwd_workspace_bytes(const Args& a)
     BwdArgs f{};
     f.a = a;
     plan(f);
-    return room(f).end;
+    return packing(a, true).end + room(f).end;
 }
 
 template <typename T, int D>
@@ -582,10 +582,13 @@ template <typename T>
 static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
 {
     const Args& a = f.a;
-    const Strides whole{(long long)a.heads * a.d, (long long)a.qm.H * a.qm.W * a.heads * a.d};
+    const Packing copies = packing(a, true);
+    hipError_t e;
+    if (copies.on && (e = pack<T>(f.a, copies, &f.dout, &f.out, ws, st)) != hipSuccess) return e;
+    ws += copies.end;
     const long long nq = (long long)a.qm.H * a.qm.W, nk = (long long)a.km.H * a.km.W;
-    f.vec = pieces(a.q, a.qs, a.d, sizeof(T), nq) && pieces(a.k, a.ks, a.d, sizeof(T), nk) && pieces(a.v, a.vs, a.d, sizeof(T), nk) &&
-            pieces(f.dout, whole, a.d, sizeof(T), nq) && pieces(f.out, whole, a.d, sizeof(T), nq);
+    f.vec = pieces(a.q, a.qs, a.dl, sizeof(T), nq) && pieces(a.k, a.ks, a.dl, sizeof(T), nk) && pieces(a.v, a.vs, a.dl, sizeof(T), nk) &&
+            pieces(f.dout, a.os, a.dl, sizeof(T), nq) && pieces(f.out, a.os, a.dl, sizeof(T), nq);
     plan(f);
     const Room r = room(f);
     f.row_lse = (float*)(ws + r.lse); f.row_D = (float*)(ws + r.D); f.sorted = (int2*)(ws + r.sorted);
@@ -593,7 +596,6 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
     const uintptr_t quad = 4 * sizeof(T) - 1;
     f.vec_dq = a.d % 4 == 0 && ((uintptr_t)f.dq & quad) == 0;
     f.vec_dk = a.d % 4 == 0 && ((uintptr_t)f.dk & quad) == 0 && ((uintptr_t)f.dv & quad) == 0;
-    hipError_t e;
     e = a.d <= 32 ? run_rows<T, 32>(f, st) : a.d <= 64 ? run_rows<T, 64>(f, st) : run_rows<T, 128>(f, st);
     if (e != hipSuccess) return e;
     // (196 entries: 5.5 us by one wave, 8.3 by four; 16384: 109 by one, 19 by four, 12 by sixteen)

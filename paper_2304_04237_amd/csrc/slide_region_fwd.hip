@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
             const long long n_px = (long long)a.qm.H * a.qm.W;
             out_at[n] = px < 0 ? -1 : ((long long)b * n_px + px) * a.heads * a.d + head * a.d;
             lse_at[n] = px < 0 ? -1 : (((long long)b * a.heads + head) * n_px + px) * 2 + ok;      // (lowest bit: the row is valid)
-            load_operand<T, D, VEC>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px : 0) * a.qs.pixel + head * a.d, ok, a.d, h);
+            load_operand<T, D, VEC>(q[n], (const T*)a.q + b * a.qs.image + (ok ? px : 0) * a.qs.pixel + head * a.hd, ok, a.dl, h);
         }
     }
     const uint32_t call = DROP ? a.rnd.call() : 0;
@@ -90,8 +90,8 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         for (int dt = 0; dt < D / 32; ++dt) o[n][dt] = f16v{};
     }
 
-    const T* kp = (const T*)a.k + b * a.ks.image + m * a.d;
-    const T* vp = (const T*)a.v + b * a.vs.image + m * a.d;
+    const T* kp = (const T*)a.k + b * a.ks.image + m * a.hd;
+    const T* vp = (const T*)a.v + b * a.vs.image + m * a.hd;
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
@@ -104,16 +104,16 @@ __global__ __launch_bounds__(256) void region_fwd_kernel(FwdArgs f)
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
         next_ok = (uint32_t)__ballot(px >= 0);
         if (DROP) next_word = (uint32_t)region * a.quads + (walk.place >> 2);
-        k.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.d, lane);
-        v.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.d, lane);
+        k.template load<VEC>(kp, row_offset<VEC, T>(px, a.ks.pixel, 0), a.dl, lane);
+        v.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.dl, lane);
     };
     fetch();
     region = walk.look(a, first + 32 + col, end);
     for (int x = first; x < end; x += 32) {
         ok = next_ok; word = next_word;
         wave_order();
-        k.stage(tile_k, ok, a.d, lane);
-        v.stage(tile_v, ok, a.d, lane);
+        k.stage(tile_k, ok, a.dl, lane);
+        v.stage(tile_v, ok, a.dl, lane);
         wave_order();
         fetch();
         region = walk.look(a, x + 64 + col, end);
@@ -292,7 +292,7 @@ static int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 size_t fwd_workspace_bytes(const Args& a)
 {
     const Cut c = cut(a);
-    return c.shares > 1 ? (size_t)a.B * a.kv * a.qm.regions * c.tiles * c.shares * (padded(a.d) * 32 + 64) * sizeof(float) : 0;
+    return packing(a, false).end + (c.shares > 1 ? (size_t)a.B * a.kv * a.qm.regions * c.tiles * c.shares * (padded(a.d) * 32 + 64) * sizeof(float) : 0);
 }
 
 template <typename T, int D>
@@ -334,11 +334,17 @@ static hipError_t run(FwdArgs& f, hipStream_t st)
 }
 
 template <typename T>
-static hipError_t run_t(FwdArgs& f, hipStream_t st)
+static hipError_t run_t(FwdArgs& f, unsigned char* ws, hipStream_t st)
 {
     const Args& a = f.a;
+    const Packing copies = packing(a, false);
+    if (copies.on) {
+        const hipError_t e = pack<T>(f.a, copies, nullptr, nullptr, ws, st);
+        if (e != hipSuccess) return e;
+    }
+    f.part = (float*)(ws + copies.end);
     const long long nq = (long long)a.qm.H * a.qm.W, nk = (long long)a.km.H * a.km.W;
-    f.vec = pieces(a.q, a.qs, a.d, sizeof(T), nq) && pieces(a.k, a.ks, a.d, sizeof(T), nk) && pieces(a.v, a.vs, a.d, sizeof(T), nk);
+    f.vec = pieces(a.q, a.qs, a.dl, sizeof(T), nq) && pieces(a.k, a.ks, a.dl, sizeof(T), nk) && pieces(a.v, a.vs, a.dl, sizeof(T), nk);
     f.vec_o = a.d % 4 == 0 && ((uintptr_t)f.out & (4 * sizeof(T) - 1)) == 0;
     const Cut c = cut(a);
     if (c.split) return a.d <= 32 ? run_split<T, 32>(f, c, st) : a.d <= 64 ? run_split<T, 64>(f, c, st) : run_split<T, 128>(f, c, st);
@@ -353,9 +359,9 @@ static hipError_t run_t(FwdArgs& f, hipStream_t st)
 hipError_t launch_fwd(const Args& a, void* out, float* lse, void* workspace, hipStream_t st)
 {
     FwdArgs f{};
-    f.a = a; f.out = out; f.lse = lse; f.part = (float*)workspace;
+    f.a = a; f.out = out; f.lse = lse;
     f.slots = 4 * a.quads * a.T;
-    return a.dtype == 0 ? run_t<float>(f, st) : run_t<bf16_bits>(f, st);
+    return a.dtype == 0 ? run_t<float>(f, (unsigned char*)workspace, st) : run_t<bf16_bits>(f, (unsigned char*)workspace, st);
 }
 
 }  // namespace region

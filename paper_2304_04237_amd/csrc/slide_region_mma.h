@@ -342,6 +342,81 @@ inline bool pieces(const void* p, const Strides& s, int d, size_t esz, long long
     return ((uintptr_t)p & 15) == 0 && s.pixel % n == 0 && s.image % n == 0 && d % n == 0 && pixels * (s.pixel / n) < (1ll << 32) - 65536;
 }
 
+// Copies of q, k, v (dout, out) whose heads are whole pieces, zeros behind d, for head sizes and strides that are not.  One launch; the products'
+// kernels then load whole pieces (9 lists of 16 from 204 x 267 pixels, heads of 17: 2190 us without).
+struct Copies {
+    const void* from[5];
+    void* to[5];
+    Strides strides[5];
+    int heads[5];
+    long long pixels[5], first[6];          // of an image; first piece of each tensor in the launch
+    int n, d, dp;
+};
+
+template <typename T>
+static __global__ __launch_bounds__(256) void region_copy_kernel(Copies f)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    typedef decltype(gather_piece((const T*)nullptr, 0)) Piece;
+    const int pieces = f.dp / E;
+    for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < f.first[f.n]; at += (long long)gridDim.x * 256) {
+        int t = 0;
+        while (at >= f.first[t + 1]) ++t;
+        const long long x = at - f.first[t], head = x / pieces, pixel = head / f.heads[t], b = pixel / f.pixels[t];
+        const int c = (int)(x - head * pieces) * E, h = (int)(head - pixel * f.heads[t]);
+        const T* from = (const T*)f.from[t] + b * f.strides[t].image + (pixel - b * f.pixels[t]) * f.strides[t].pixel + h * f.d + c;
+        ((Piece*)f.to[t])[x] = gather_piece(from, f.d - c);
+    }
+}
+
+// Whether a call works on copies, and the workspace's bytes for them.  Not where fewer keys are attended than there are (one token over a
+// long sequence): then the kernels gather the elements themselves, as they do for tensors that are merely not aligned.
+struct Packing { bool on; int dp; size_t bytes[5], end; };
+
+inline Packing packing(const Args& a, bool backward)
+{
+    const int esz = a.dtype == 0 ? 4 : 2, E = 16 / esz;
+    Packing p{};
+    p.dp = (a.d + E - 1) / E * E;
+    const long long nq = (long long)a.qm.H * a.qm.W, nk = (long long)a.km.H * a.km.W;
+    bool whole = a.d % E == 0;
+    for (const Strides& s : {a.qs, a.ks, a.vs}) whole = whole && s.pixel % E == 0 && s.image % E == 0;
+    const bool often = backward || (long long)a.qm.regions * a.T * a.km.places >= nk;
+    const bool small = std::max(nq * a.heads, nk * a.kv) * (p.dp / E) < (1ll << 32) - 65536;
+    p.on = !whole && often && small;
+    for (int t = 0; t < 5 && p.on; ++t) {
+        p.bytes[t] = t >= 3 && !backward ? 0 : ((size_t)a.B * (t == 1 || t == 2 ? nk * a.kv : nq * a.heads) * p.dp * esz + 255) / 256 * 256;
+        p.end += p.bytes[t];
+    }
+    return p;
+}
+
+// Makes the copies at ws and has a (dout, out) refer to them
+template <typename T>
+static hipError_t pack(Args& a, const Packing& p, const void** dout, const void** out, unsigned char* ws, hipStream_t st)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    Copies f{};
+    f.n = dout ? 5 : 3; f.d = a.d; f.dp = p.dp;
+    const void* from[5] = {a.q, a.k, a.v, dout ? *dout : nullptr, out ? *out : nullptr};
+    Strides* strides[5] = {&a.qs, &a.ks, &a.vs, &a.os, &a.os};
+    for (int t = 0; t < f.n; ++t) {
+        const bool keys = t == 1 || t == 2;
+        f.from[t] = from[t]; f.to[t] = ws; f.strides[t] = *strides[t];
+        f.heads[t] = keys ? a.kv : a.heads;
+        f.pixels[t] = keys ? (long long)a.km.H * a.km.W : (long long)a.qm.H * a.qm.W;
+        f.first[t + 1] = f.first[t] + a.B * f.pixels[t] * f.heads[t] * (p.dp / E);
+        ws += p.bytes[t];
+    }
+    for (int t = 0; t < f.n; ++t) *strides[t] = Strides{(long long)f.heads[t] * p.dp, f.pixels[t] * f.heads[t] * p.dp};
+    a.q = f.to[0]; a.k = f.to[1]; a.v = f.to[2];
+    if (dout) { *dout = f.to[3]; *out = f.to[4]; }
+    a.hd = a.dl = p.dp;
+    const long long blocks = (f.first[f.n] + 255) / 256;
+    region_copy_kernel<T><<<(int)std::min<long long>(blocks, 1 << 20), 256, 0, st>>>(f);
+    return hipGetLastError();
+}
+
 // Workgroups go to the eight XCDs in turn, each with an L2 of its own: work items that share keys are given to one XCD in a row.
 __device__ __forceinline__ uint32_t xcd_order(uint32_t block, uint32_t blocks)
 {

@@ -206,15 +206,18 @@ def _on_device(call):
 
 
 @_on_device
-def _region_workspace_bytes(q, k, code, topk, heads, q_region, k_region, kv_heads):
-    maps = (("k", k), ("v", k))
+def _region_workspace_bytes(q, k, v, code, topk, heads, q_region, k_region, kv_heads):
+    maps = (("k", k), ("v", v))
     plan = _plan(q, maps, heads, q_region, k_region, kv_heads, topk)
     return int(_library().slide_region_workspace_bytes(plan.problem(None, None, _device(q, maps)), code))
 
 
-def slide_region_workspace_bytes(call, q, k, topk, heads, q_region, k_region, kv_heads=None):
-    """Bytes of scratch of slide_region_select ("select"), slide_region_attn_fwd ("fwd") or slide_region_attn_bwd ("bwd")."""
-    return _region_workspace_bytes(q, k, {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call], topk, heads, q_region, k_region, kv_heads)
+def slide_region_workspace_bytes(call, q, k, topk, heads, q_region, k_region, kv_heads=None, v=None):
+    """Bytes of scratch of slide_region_select ("select"), slide_region_attn_fwd ("fwd") or slide_region_attn_bwd ("bwd").
+
+    v: where its strides are not those of k."""
+    code = {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call]
+    return _region_workspace_bytes(q, k, k if v is None else v, code, topk, heads, q_region, k_region, kv_heads)
 
 
 @_on_device

@@ -42,6 +42,8 @@ CASES = {
     "list_ends_early": case((20, 20), B=2, heads=2, d=32, q_region=(5, 5), topk=70, lists="early"),
     "one_token_128_channels_many_keys": case((1, 1), (1, 9000), B=2, heads=8, kv_heads=2, d=128, q_region=(1, 1), k_region=(1, 64), topk=60, sized=True),
     "map_as_one_region": case((30, 31), heads=1, d=32, q_region=(99, 99), k_region=(99, 99), topk=1, lists="all"),
+    "odd_channels_few_keys_attended": case((6, 7), (40, 50), heads=2, d=33, q_region=(6, 7), k_region=(5, 5), topk=2),
+    "60_channels": case((18, 15), B=2, heads=3, d=60, q_region=(6, 3), topk=9, sized=True),
     "scale": case((8, 8), d=32, q_region=(4, 4), topk=2, scale=0.7),
     "steep": case((8, 8), d=32, q_region=(4, 4), topk=2, scale=3.0),
     "dropped_ragged": case((13, 19), B=2, heads=3, d=24, q_region=(4, 5), sized=True, dropout=0.3),
@@ -196,13 +198,14 @@ def test_the_same_twice_and_on_another_stream(name):
         assert torch.equal(a.nan_to_num(), b.nan_to_num())
 
 
-def test_outputs_and_workspaces_of_the_caller():
+@pytest.mark.parametrize("name", ["dropped_ragged", "odd_channels", "one_token_many_keys"])
+def test_outputs_and_workspaces_of_the_caller(name):
     """Given outputs are written whole, and nothing behind a workspace of exactly the size asked for."""
-    c = CASES["dropped_ragged"]
+    c = CASES[name]
     t, index, how = make(c, "bf16", seed=8)
     g, idx, gh = on_gpu(t, index, how)
-    sizes = {n: gh.pop(n) for n in ("q_size", "k_size")}
-    drop = {n: gh.pop(n) for n in ("dropout", "seed", "offset")}
+    sizes = {n: gh.pop(n) for n in ("q_size", "k_size") if n in gh}
+    drop = {n: gh.pop(n) for n in ("dropout", "seed", "offset") if n in gh}
     out, lse = forward(g, idx, dict(gh, **sizes, **drop))
     want = backward(g, idx, dict(gh, **sizes, **drop), out, lse)
 
