@@ -55,14 +55,15 @@ template <> __device__ __forceinline__ float piece_dot<float>(const u4& a, const
 // dq and, for the key kernel, every row's lse and D.
 // bf16: out was rounded, so dout.out is off by up to 2^-8 of its terms.  The sum of P F dP, which is D without that, is only known at
 // the end; until then the rounded D0 is used, and dq is corrected by (D - D0) sum P k, for one more product.
-template <typename T, int D, bool DROP, bool VEC>
+// SPLIT: the four waves of a block take a quarter each of the keys of the same rows and add their sums in LDS.
+template <typename T, int D, bool DROP, bool SPLIT, bool VEC>
 __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
 {
     constexpr bool FIX = sizeof(T) == 2;
     const Args& a = f.a;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int item = (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
+    const int item = SPLIT ? (int)xcd_order(blockIdx.x, gridDim.x) : (int)xcd_order(blockIdx.x, gridDim.x) * 4 + wave;
     if (item >= f.items) return;
     unsigned char* tile_k = lds + wave * 2 * Tile<T, D>::BYTES;
     unsigned char* tile_v = tile_k + Tile<T, D>::BYTES;
@@ -112,9 +113,14 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
     Walk walk;
     walk.list = a.index + (long long)group * a.T;
     a.km.limits(b, walk.vh, walk.vw);
-    const int slots = walk.length(a);
+    int first = 0, slots = walk.length(a);
+    if (SPLIT) {
+        const int tiles = (slots + 31) / 32;
+        first = tiles * wave / 4 * 32;
+        slots = min(slots, tiles * (wave + 1) / 4 * 32);
+    }
     Rows<T, D> kn, vn;
-    int region = walk.look(a, col, slots);
+    int region = walk.look(a, first + col, slots);
     uint32_t next_word = 0, next_ok;
     auto fetch = [&]() {
         const int px = Walk::pixel(a, region, walk.place, walk.vh, walk.vw);
@@ -124,8 +130,8 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         vn.template load<VEC>(vp, row_offset<VEC, T>(px, a.vs.pixel, 0), a.dl, lane);
     };
     fetch();
-    region = walk.look(a, 32 + col, slots);
-    for (int x = 0; x < slots; x += 32) {
+    region = walk.look(a, first + 32 + col, slots);
+    for (int x = first; x < slots; x += 32) {
         const uint32_t ok = next_ok, word = next_word;
         wave_order();
         kn.stage(tile_k, ok, a.dl, lane);
@@ -164,29 +170,61 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
         accumulate<D, NA>(acc, tile_k, w, lane);
     }
 
-    const float exact = FIX ? halves_sum(D1) : D0, fix = exact - D0;
-    if (h == 0) {
+    float exact = FIX ? halves_sum(D1) : D0;
+    float* sums = (float*)lds;                      // SPLIT: [wave][D][32], then the waves' parts of D
+    if constexpr (SPLIT) {
+        __syncthreads();                            // (the tiles are in the same place)
+        if (FIX) {
+            float* D_of = sums + 4 * D * 32;
+            if (h == 0) D_of[wave * 32 + col] = exact;
+            __syncthreads();
+            exact = (D_of[col] + D_of[32 + col]) + (D_of[64 + col] + D_of[96 + col]);
+        }
+    }
+    const float fix = exact - D0;
+    if (h == 0 && (!SPLIT || wave == 0)) {
         const long long at = (long long)group * f.row_tiles * 32 + r;
         f.row_lse[at] = row_lse;
         f.row_D[at] = exact;
     }
-    if (out_at < 0) return;
     const bool valid = row_lse != INFINITY;
     const float up = a.scale * keep;
+    if (FIX) {
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
+        for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int u = 0; u < 16; u += 4) {
-            const int c = 32 * dt + acc_row(u, h);
+            for (int u = 0; u < 16; ++u) acc[0][dt][u] = __builtin_fmaf(-fix, acc[NA - 1][dt][u], acc[0][dt][u]);
+    }
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int u = 0; u < 16; ++u) sums[(wave * D + 32 * dt + acc_row(u, h)) * 32 + col] = acc[0][dt][u];
+        __syncthreads();
+        if (out_at < 0) return;
+        for (int c = 4 * (threadIdx.x >> 5); c < D; c += 32) {
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[e] = acc[0][dt][u + e];
-                if (FIX) x[e] = __builtin_fmaf(-fix, acc[NA - 1][dt][u + e], x[e]);
+                const float* s = sums + (c + e) * 32 + col;
+                x[e] = (s[0] + s[D * 32]) + (s[2 * D * 32] + s[3 * D * 32]);
                 x[e] = valid ? x[e] * up : 0.0f;
             }
             store4((T*)f.dq + out_at + c, x, a.d - c, f.vec_dq);
         }
+    } else {
+        if (out_at < 0) return;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int u = 0; u < 16; u += 4) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = valid ? acc[0][dt][u + e] * up : 0.0f;
+                const int c = 32 * dt + acc_row(u, h);
+                store4((T*)f.dq + out_at + c, x, a.d - c, f.vec_dq);
+            }
+    }
 }
 
 // The lists turned around: a wave per region of keys (or sixteen, each over its part, where the lists are long)
@@ -466,7 +504,7 @@ __global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3
         }
 }
 
-// The regions that more than `share` groups list: adds up the float32 sums of their waves, in order.
+// The regions that more than `share` groups list: adds up the float32 sums of their waves, in order; twice four channels of a key a thread.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
 {
@@ -482,12 +520,14 @@ __global__ __launch_bounds__(256) void region_dkdv_join_kernel(BwdArgs f)
     if (s / f.share != window || e - s <= f.share) return;
     const float* part = f.partial + ((long long)bm * f.key_tiles + kt) * 2 * f.windows * (2 * 32 * D);
     const int last = (e - 1) / f.share;
-    for (int u = threadIdx.x; u < 2 * 32 * D / 4; u += 256) {
-        f4 sum = *(const f4*)(part + (long long)(2 * window) * (2 * 32 * D) + 4 * u);
-        for (int w = (s + f.share) / f.share; w <= last; ++w) sum += *(const f4*)(part + (long long)(2 * w + 1) * (2 * 32 * D) + 4 * u);
+#pragma unroll
+    for (int u = blockIdx.y * 512 + threadIdx.x, n = 0; n < 2; ++n, u += 256) {
         const int c = 4 * u % D, place = kt * 32 + 4 * u / D % 32, side = 4 * u / D / 32;
         const int px = place < a.km.places ? a.km.pixel(j, place, a.km.H, a.km.W) : -1;
         if (px < 0) continue;
+        f4 sum = *(const f4*)(part + (long long)(2 * window) * (2 * 32 * D) + 4 * u);
+#pragma unroll 4
+        for (int w = (s + f.share) / f.share; w <= last; ++w) sum += *(const f4*)(part + (long long)(2 * w + 1) * (2 * 32 * D) + 4 * u);
         const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
         store4((T*)(side ? f.dv : f.dk) + ((long long)b * a.km.H * a.km.W + px) * a.kv * a.d + m * a.d + c, x, a.d - c, f.vec_dk);
     }
@@ -509,9 +549,11 @@ static void plan(BwdArgs& f)
     // against 218 us); with few, as at stage 1 (8), the joining costs more than the finer division gives.
     const long long average = ((long long)f.entries + a.km.regions - 1) / a.km.regions;
     f.team = average * slots >= 24 * 32 ? 4 : 1;
-    // A block's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip
+    // A block's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip, but
+    // four row tiles, for less costs more in sums that are written and joined than it gains (28 x 46, regions of 13 x 5, heads of 128:
+    // 74 us with one entry a block, 45 so; float32, 38 x 53: 289 and 181), and heads of 128, of which a SIMD holds one wave, fill the chip with fewer.
     const long long all = (long long)a.B * a.kv * f.key_tiles * f.entries * f.team;
-    const long long fill = std::max((long long)f.team, all / (16ll * device_cu_count()));
+    const long long fill = std::max({(long long)f.team, all / ((a.d > 64 ? 4ll : 16ll) * device_cu_count()), (4 * 32 * f.team + slots - 1) / slots});
     f.share = (int)std::min({std::max(2 * average, (8 * 32 + slots - 1) / slots), fill, (1ll << 30) / slots});
     f.windows = (f.entries + f.share - 1) / f.share;
 }
@@ -545,13 +587,20 @@ template <typename T, int D>
 static hipError_t run_rows(BwdArgs& f, hipStream_t st)
 {
     f.items = f.a.B * f.a.kv * f.a.qm.regions * f.row_tiles;
-    const int blocks = (f.items + 3) / 4, lds = 8 * Tile<T, D>::BYTES;
+    // SPLIT where a wave per 32 rows would not give every SIMD one (50 x 47, 448 waves over 2500 keys: 70 us, split 29), and with
+    // heads of 128, of which a SIMD holds one wave, or half of them (704 waves of float32: 67 us, split 111).
+    const bool split = f.items < (D == 128 ? 2 : 4) * device_cu_count() && f.slots > 4 * 32;
+    const int blocks = split ? f.items : (f.items + 3) / 4, lds = split ? std::max(8 * Tile<T, D>::BYTES, 4 * D * 32 * 4 + 512) : 8 * Tile<T, D>::BYTES;
     static LdsOptIn opt;
-    const hipError_t e = opt.ensure({(const void*)region_dq_kernel<T, D, true, false>, (const void*)region_dq_kernel<T, D, true, true>,
-                                     (const void*)region_dq_kernel<T, D, false, true>}, lds);
+    const hipError_t e = opt.ensure({(const void*)region_dq_kernel<T, D, true, false, false>, (const void*)region_dq_kernel<T, D, true, false, true>,
+                                     (const void*)region_dq_kernel<T, D, false, false, true>, (const void*)region_dq_kernel<T, D, true, true, false>,
+                                     (const void*)region_dq_kernel<T, D, true, true, true>, (const void*)region_dq_kernel<T, D, false, true, true>},
+                                    std::max(8 * Tile<T, D>::BYTES, 4 * D * 32 * 4 + 512));
     if (e != hipSuccess) return e;
     // (what is not in whole pieces takes the kernels with dropout, which drop nothing below a threshold of 0)
-    const auto kernel = !f.vec ? region_dq_kernel<T, D, true, false> : f.a.rnd.threshold ? region_dq_kernel<T, D, true, true> : region_dq_kernel<T, D, false, true>;
+    const auto kernel = !f.vec ? (split ? region_dq_kernel<T, D, true, true, false> : region_dq_kernel<T, D, true, false, false>)
+                      : f.a.rnd.threshold ? (split ? region_dq_kernel<T, D, true, true, true> : region_dq_kernel<T, D, true, false, true>)
+                                          : (split ? region_dq_kernel<T, D, false, true, true> : region_dq_kernel<T, D, false, false, true>);
     kernel<<<blocks, 256, lds, st>>>(f);
     return hipGetLastError();
 }
@@ -572,7 +621,7 @@ static hipError_t run_keys(BwdArgs& f, hipStream_t st)
     kernel<<<(int)items, 64 * f.team, lds, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (f.entries > f.share) {
-        region_dkdv_join_kernel<T, D><<<f.a.B * f.a.kv * f.key_tiles * f.windows, 256, 0, st>>>(f);
+        region_dkdv_join_kernel<T, D><<<dim3(f.a.B * f.a.kv * f.key_tiles * f.windows, D / 32), 256, 0, st>>>(f);
         e = hipGetLastError();
     }
     return e;

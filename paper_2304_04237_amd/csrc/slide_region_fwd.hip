@@ -271,8 +271,8 @@ __global__ __launch_bounds__(256) void region_fwd_join_kernel(FwdArgs f)
 }
 
 // How a problem is cut.  A block per 32 rows and share of the keys (SPLIT) where a wave per 32 rows would not give every SIMD one (8 new
-// tokens, 32 heads of 128 over 4096 keys: 236 us by 32 waves, 28 split); then as many shares as give every SIMD one wave, of at
-// least two key tiles each.
+// tokens, 32 heads of 128 over 4096 keys: 236 us by 32 waves, 28 split), and for heads of 128 half of them (704 waves of float32: 53 us, split
+// 87); then as many shares as give every SIMD one wave, of at least eight key tiles each.
 struct Cut { bool split; int tiles, shares; };
 
 static Cut cut(const Args& a)
@@ -282,7 +282,7 @@ static Cut cut(const Args& a)
     Cut c{false, (a.R + 31) / 32, 1};
     const long long items = groups * c.tiles;
     const int key_tiles = (4 * a.quads * a.T + 31) / 32;
-    c.split = items < 4ll * cus && key_tiles > 1;
+    c.split = items < (a.d > 64 ? 2ll : 4ll) * cus && key_tiles > 1;
     if (c.split) c.shares = (int)std::max(1ll, std::min((cus + items - 1) / items, (long long)key_tiles / 8));
     return c;
 }

@@ -41,6 +41,10 @@ CASES = {
     "1024_entries": case((1, 70), (1, 300), heads=2, d=32, q_region=(1, 35), k_region=(1, 2), topk=1024),
     "list_ends_early": case((20, 20), B=2, heads=2, d=32, q_region=(5, 5), topk=70, lists="early"),
     "one_token_128_channels_many_keys": case((1, 1), (1, 9000), B=2, heads=8, kv_heads=2, d=128, q_region=(1, 1), k_region=(1, 64), topk=60, sized=True),
+    "1088_groups": case((64, 68), heads=4, d=32, q_region=(4, 4), topk=10, sized=True),
+    "624_groups_128_channels": case((48, 50), heads=4, d=128, q_region=(4, 4), topk=9),
+    "dropped_1088_groups": case((64, 68), heads=4, d=24, q_region=(4, 4), topk=10, dropout=0.2),
+    "dropped_two_of_many_regions": case((12, 12), heads=2, d=64, q_region=(6, 6), k_region=(5, 5), topk=9, dropout=0.4, sized=True),
     "map_as_one_region": case((30, 31), heads=1, d=32, q_region=(99, 99), k_region=(99, 99), topk=1, lists="all"),
     "odd_channels_few_keys_attended": case((6, 7), (40, 50), heads=2, d=33, q_region=(6, 7), k_region=(5, 5), topk=2),
     "60_channels": case((18, 15), B=2, heads=3, d=60, q_region=(6, 3), topk=9, sized=True),
@@ -180,6 +184,31 @@ def test_parts_of_wider_tensors(dtype):
     assert torch.equal(a[0], b[0])
     for u, w in zip(backward(one, idx, gh, *a), backward(same, idx, gh, *b)):
         assert torch.equal(u, w)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["regions_7x7", "100_channels", "many_small_regions", "64_channels", "1088_groups", "dropped_stage_like",
+                                  "dropped_two_of_many_regions", "dropped_128_channels", "dropped_sequence"])
+def test_tensors_that_begin_anywhere(name, dtype):
+    """Whole strides behind an address that is no multiple of 16 bytes, for inputs and for the gradients' own memory."""
+    c = CASES[name]
+    t, index, how = make(c, dtype, seed=12)
+    print(name, dtype, flush=True)
+    x = clean(t)
+    ref = ro.attention(x["q"], x["k"], x["v"], index, how, x["dout"])
+    g, idx, gh = on_gpu(t, index, how)
+
+    def moved(x):
+        room = torch.full((x.numel() + 1,), float("nan"), dtype=x.dtype, device="cuda")
+        room[1:].copy_(x.reshape(-1))
+        return room[1:].view(x.shape)
+
+    g = {n: moved(x) for n, x in g.items()}
+    out, lse = forward(g, idx, gh)
+    grads = backward(g, idx, gh, moved(out), lse)
+    bound = bounds(c, dtype, ref)
+    for n, got in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+        assert (np.abs(numpy_of(got) - ref[n]) / bound[n]).max() <= 1, n
 
 
 @pytest.mark.parametrize("name", ["ragged_24_channels", "one_token_many_keys", "everyone_lists_the_same", "600_lists_64_channels", "dropped_sequence"])
