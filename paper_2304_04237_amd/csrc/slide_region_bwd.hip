@@ -227,50 +227,71 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
     }
 }
 
-// The lists turned around: a wave per region of keys (or sixteen, each over its part, where the lists are long)
-// goes over all entries of its image and head, first counting, then writing in order.
+// The lists turned around: a wave per region of keys, or sixteen, each over its part, per N regions where the lists are long, go over
+// all entries of their image and head, first counting, then writing in order.
+template <int N>
 __global__ __launch_bounds__(1024) void region_invert_kernel(BwdArgs f)
 {
     const Args& a = f.a;
-    __shared__ int2 counts[16];
-    const int lane = threadIdx.x & 63, J = a.km.regions;
+    __shared__ int less_of[16], mine_of[16][N];
+    const int lane = threadIdx.x & 63, J = a.km.regions, units = (J + N - 1) / N;
     const int waves = f.invert_waves, wave = (threadIdx.x >> 6) & (waves - 1), base = (threadIdx.x >> 6) - wave;
     const long long id = waves == 1 ? (long long)blockIdx.x * 4 + base : blockIdx.x;
-    const bool live = id < (long long)a.B * a.kv * J;
-    const int bm = live ? (int)(id / J) : 0, j = live ? (int)(id - (long long)bm * J) : -1;
+    const bool live = id < (long long)a.B * a.kv * units;
+    const int bm = live ? (int)(id / units) : 0, j = live ? (int)(id - (long long)bm * units) * N : 0;
     const int* list = a.index + (long long)bm * f.entries;
     const int run = (f.entries + 64 * waves - 1) / (64 * waves) * 64;
     const int first = min(wave * run, f.entries), end = live ? min(first + run, f.entries) : 0;
-    int less = 0, mine = 0;
+    int less = 0, mine[N] = {};
 #pragma unroll 8
     for (int e = first + lane; e < end; e += 64) {
         const int x = list[e];
-        less += x >= 0 && x < j;
-        mine += x == j;
+        less += (uint32_t)x < (uint32_t)j;
+#pragma unroll
+        for (int n = 0; n < N; ++n) mine[n] += x == j + n;
     }
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) { less += __shfl_xor(less, s); mine += __shfl_xor(mine, s); }
-    if (lane == 0) counts[base + wave] = int2{less, mine};
+    for (int s = 32; s > 0; s >>= 1) {
+        less += __shfl_xor(less, s);
+#pragma unroll
+        for (int n = 0; n < N; ++n) mine[n] += __shfl_xor(mine[n], s);
+    }
+    if (lane == 0) {
+        less_of[base + wave] = less;
+#pragma unroll
+        for (int n = 0; n < N; ++n) mine_of[base + wave][n] = mine[n];
+    }
     __syncthreads();
     if (!live) return;
-    int at = 0, total = 0;
-    for (int w = 0; w < waves; ++w) {
-        at += counts[base + w].x + (w < wave ? counts[base + w].y : 0);
-        total += counts[base + w].y;
+    int at = 0, hits = 0;
+    int2* to[N];
+    for (int w = 0; w < waves; ++w) at += less_of[base + w];
+    int* start = f.start + (long long)bm * (J + 1);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (wave == 0 && lane == 0 && j + n < J) start[j + n] = at;
+        int before = 0, all = 0;
+        for (int w = 0; w < waves; ++w) {
+            before += w < wave ? mine_of[base + w][n] : 0;
+            all += mine_of[base + w][n];
+        }
+        to[n] = f.sorted + (long long)bm * f.entries + at + before;
+        if (j + n < J) { at += all; hits += mine[n]; }
     }
-    if (wave == 0 && lane == 0) {
-        f.start[(long long)bm * (J + 1) + j] = at;
-        if (j == J - 1) f.start[(long long)bm * (J + 1) + J] = at + total;
-    }
-    if (counts[base + wave].y == 0) return;
-    int2* to = f.sorted + (long long)bm * f.entries + at;
+    if (wave == 0 && lane == 0 && j + N >= J) start[J] = at;
+    if (hits == 0) return;
+    const int last = min(j + N, J);
 #pragma unroll 4
     for (int e0 = first; e0 < end; e0 += 64) {
-        const int e = e0 + lane;
-        const bool hit = e < end && list[e] == j;
-        const uint64_t mask = __ballot(hit);
-        if (hit) to[__popcll(mask & ((1ull << lane) - 1))] = int2{e / a.T, j};
-        to += __popcll(mask);
+        const int e = e0 + lane, x = e < end ? list[e] : -1;
+        if (!__ballot(x >= j && x < last)) continue;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const bool hit = x == j + n && j + n < last;
+            const uint64_t mask = __ballot(hit);
+            if (hit) to[n][__popcll(mask & ((1ull << lane) - 1))] = int2{e / a.T, x};
+            to[n] += __popcll(mask);
+        }
     }
 }
 
@@ -649,9 +670,11 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
     if (e != hipSuccess) return e;
     // (196 entries: 5.5 us by one wave, 8.3 by four; 16384: 109 by one, 19 by four, 12 by sixteen)
     f.invert_waves = f.entries >= 2048 ? 16 : 1;
-    const int regions = a.B * a.kv * a.km.regions;
-    if (f.invert_waves == 1) region_invert_kernel<<<(regions + 3) / 4, 256, 0, st>>>(f);
-    else region_invert_kernel<<<regions, 1024, 0, st>>>(f);
+    const int lists = a.B * a.kv, regions = lists * a.km.regions;
+    // Four regions a block where that still fills the chip (8262 regions: 77 us by one, 46 by four; 312: 9.5 and 14).
+    if (f.invert_waves == 1) region_invert_kernel<1><<<(regions + 3) / 4, 256, 0, st>>>(f);
+    else if (regions < 4 * device_cu_count()) region_invert_kernel<1><<<regions, 1024, 0, st>>>(f);
+    else region_invert_kernel<4><<<lists * ((a.km.regions + 3) / 4), 1024, 0, st>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return a.d <= 32 ? run_keys<T, 32>(f, st) : a.d <= 64 ? run_keys<T, 64>(f, st) : run_keys<T, 128>(f, st);
 }

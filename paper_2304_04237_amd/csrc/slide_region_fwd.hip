@@ -349,8 +349,10 @@ static hipError_t run_t(FwdArgs& f, unsigned char* ws, hipStream_t st)
     const Cut c = cut(a);
     if (c.split) return a.d <= 32 ? run_split<T, 32>(f, c, st) : a.d <= 64 ? run_split<T, 64>(f, c, st) : run_split<T, 128>(f, c, st);
     // Two row tiles per wave load and stage every key half as often, where the registers hold them (bf16; one tile: 2 x 200 x 333
-    // pixels, heads of 32: 130 against 115 us; 16384 tokens, heads of 64: 95 against 72)
-    const bool two = a.R > 32 && f.vec;
+    // pixels, heads of 32: 130 against 115 us; 16384 tokens, heads of 64: 95 against 72).  With heads of 32 an odd tile left over costs more than
+    // that where there are few (50 x 40 x 48 pixels, 80 rows: 102 us by two, 80 by one).
+    const int tiles = (a.R + 31) / 32;
+    const bool two = a.R > 32 && f.vec && !(a.d <= 32 && tiles < 8 && tiles % 2);
     if (a.d <= 32) return two ? run<T, 32, 2>(f, st) : run<T, 32, 1>(f, st);
     if (a.d <= 64) return two && sizeof(T) == 2 ? run<T, 64, 2>(f, st) : run<T, 64, 1>(f, st);
     return run<T, 128, 1>(f, st);
