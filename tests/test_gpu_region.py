@@ -45,8 +45,8 @@ CASES = {
     "624_groups_128_channels": case((48, 50), heads=4, d=128, q_region=(4, 4), topk=9),
     "dropped_1088_groups": case((64, 68), heads=4, d=24, q_region=(4, 4), topk=10, dropout=0.2),
     "dropped_two_of_many_regions": case((12, 12), heads=2, d=64, q_region=(6, 6), k_region=(5, 5), topk=9, dropout=0.4, sized=True),
-    "2054_regions_2600_entries": case((1, 650), (1, 2054), B=1, heads=1, d=16, q_region=(1, 1), k_region=(1, 1), topk=4),
-    "lists_among_1027_regions": case((1, 300), (1, 1027), B=2, heads=2, d=16, q_region=(1, 2), k_region=(1, 1), topk=16, sized=True),
+    "dropped_2600_entries": case((1, 650), (1, 2054), heads=1, d=16, q_region=(1, 1), k_region=(1, 1), topk=4, dropout=0.1),
+    "dropped_2400_entries_sized": case((1, 300), (1, 1027), B=2, heads=2, d=16, q_region=(1, 2), k_region=(1, 1), topk=16, sized=True, dropout=0.1),
     "map_as_one_region": case((30, 31), heads=1, d=32, q_region=(99, 99), k_region=(99, 99), topk=1, lists="all"),
     "odd_channels_few_keys_attended": case((6, 7), (40, 50), heads=2, d=33, q_region=(6, 7), k_region=(5, 5), topk=2),
     "60_channels": case((18, 15), B=2, heads=3, d=60, q_region=(6, 3), topk=9, sized=True),
