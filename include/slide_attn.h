@@ -320,6 +320,7 @@ int slide_attn_fwd_traffic_probe(const void* q, const void* k, const void* v, vo
  * q_size, k_size: int32 [B, 2] on the device or NULL: the valid height and width of every image (clamped to the map), where a
  * batch is padded at the right and bottom.  Pixels outside are never read as keys, whatever they hold; as queries they get
  * zeros (lse: -infinity) and pass nothing to any gradient.  A row that has no key at all gets the same.
+ * (The gradients of a key that is not finite are not finite either where a region with rows inside lists it.)
  * scale: of the logits; 0 stands for 1/sqrt(head_dim).
  * dropout: of the attention weights, in [0, 1); it is rounded to t / 65536, and weights that are kept are multiplied by
  * 65536 / (65536 - t).  The mask is a function of seed, offset and the weight's place, and is never stored: the backward draws

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
     if (h == 0 && (!SPLIT || wave == 0)) {
         const long long at = (long long)group * f.row_tiles * 32 + r;
         f.row_lse[at] = row_lse;
-        f.row_D[at] = exact;
+        f.row_D[at] = row_lse != INFINITY ? exact : 0.0f;        // (keys may hold anything)
     }
     const bool valid = row_lse != INFINITY;
     const float up = a.scale * keep;
@@ -401,7 +401,16 @@ __global__ __launch_bounds__(64 * TEAM, sizeof(T) == 2 && D <= 64 ? (D == 32 ? 3
     const T* gp = (const T*)f.dout + b * a.os.image;
     // The rows of the groups one after the other, each group's padded to whole pairs (a patch of the dropout counter): slot y is row
     // y % (2 pairs) of the group of entry from + y / (2 pairs), and a tile holds rows of several groups.
-    const int entries = to - from, steps = (entries * (2 * a.pairs) + 31) / 32;
+    int entries = to - from;
+    if (a.qm.size) {
+        // Nothing to do where every group lies outside its image.  (A row that does not count is zeros with a weight of zero, which is nothing
+        // unless a key is not finite; such a key's gradients are not finite either where rows that count attend it.)
+        bool any = false;
+        for (int e = lane; e - lane < entries && !any; e += 64)
+            any = __ballot(a.qm.pixel(sorted[from + min(e, entries - 1)].x, 0, qh, qw) >= 0);
+        entries = any ? entries : 0;
+    }
+    const int steps = (entries * (2 * a.pairs) + 31) / 32;
     int row = 0;                                // this lane's row of the tile that is loaded next, its entry in bounds or not
     bool there = false;
     uint32_t next_pair = 0, pair;
@@ -569,7 +578,8 @@ static void plan(BwdArgs& f)
     // Four waves per tile of keys where a region has 24 row tiles or more on average (16384 tokens, 128 row tiles per region: 155
     // against 218 us); with few, as at stage 1 (8), the joining costs more than the finer division gives.
     const long long average = ((long long)f.entries + a.km.regions - 1) / a.km.regions;
-    f.team = average * slots >= 24 * 32 ? 4 : 1;
+    // (With 2^22 tiles the chip is full anyway, and the grid's threads stay below 2^32.)
+    f.team = average * slots >= 24 * 32 && (long long)a.B * a.kv * a.km.regions * f.key_tiles < 1 << 22 ? 4 : 1;
     // A block's share: twice what a region has on average, at least 8 row tiles; less where there would be too few waves for the chip, but
     // four row tiles, for less costs more in sums that are written and joined than it gains (28 x 46, regions of 13 x 5, heads of 128:
     // 74 us with one entry a block, 45 so; float32, 38 x 53: 289 and 181), and heads of 128, of which a SIMD holds one wave, fill the chip with fewer.

@@ -172,8 +172,11 @@ _plan_of = functools.lru_cache(maxsize=4096)(_Plan)
 
 def _plan(q, maps, heads, q_region, k_region, kv_heads, topk):
     """The plan of maps q, k (and v): everything that a kernel relies on is checked once per set of sizes, the devices every time."""
-    return _plan_of(q.dtype, q.shape, q.stride(), tuple((n, t.dtype, t.shape, t.stride()) for n, t in maps), heads,
-                    tuple(q_region), tuple(k_region), kv_heads, topk)
+    try:
+        regions = tuple(q_region), tuple(k_region)
+    except TypeError:
+        raise SlideAttnError("q_region and k_region must be (height, width)") from None
+    return _plan_of(q.dtype, q.shape, q.stride(), tuple((n, t.dtype, t.shape, t.stride()) for n, t in maps), heads, *regions, kv_heads, topk)
 
 
 def _empty(t):
@@ -216,7 +219,9 @@ def slide_region_workspace_bytes(call, q, k, topk, heads, q_region, k_region, kv
     """Bytes of scratch of slide_region_select ("select"), slide_region_attn_fwd ("fwd") or slide_region_attn_bwd ("bwd").
 
     v: where its strides are not those of k."""
-    code = {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}[call]
+    code = {"select": _SELECT, "fwd": _FWD, "bwd": _BWD}.get(call)
+    if code is None:
+        raise SlideAttnError('call must be "select", "fwd" or "bwd"')
     return _region_workspace_bytes(q, k, k if v is None else v, code, topk, heads, q_region, k_region, kv_heads)
 
 

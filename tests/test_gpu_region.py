@@ -301,6 +301,30 @@ def test_values_that_are_not_finite():
         assert o[whole].isfinite().all() and lse[0, 0, 0, 32:48].isnan().all() and lse[0, 0, 0, :32].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dropout", [0.0, 0.2])
+def test_queries_outside_pass_nothing_whatever_the_keys_hold(dtype, value, dropout):
+    """Keys that only rows outside the image list, in regions wholly and partly outside."""
+    c = case((16, 16), B=2, heads=2, d=32, q_region=(8, 8), k_region=(4, 4), topk=3, dropout=dropout)
+    t, _, how = make(c, dtype, seed=13)
+    how["q_size"] = np.array([[5, 16], [16, 8]], dtype=np.int32)
+    index = np.zeros((2, 2, 4, 3), dtype=np.int32)
+    index[:, :] = [[0, 1, -1], [2, 3, 3], [4, 5, 1], [6, 7, 15]]
+    g, idx, gh = on_gpu(t, index, how)
+    want = forward(g, idx, gh)
+    want += tuple(backward(g, idx, gh, *want))
+    for b, inside in ((0, (0, 1)), (1, (0, 2))):        # regions of queries that have rows inside
+        listed = {j for i in inside for j in index[0, 0, i]}
+        for j in set(range(16)) - listed:
+            for n in ("k", "v"):
+                g[n][b, 4 * (j // 4), 4 * (j % 4) + 1] = value
+    got = forward(g, idx, gh)
+    got += tuple(backward(g, idx, gh, *got))
+    for a, w in zip(got, want):
+        assert torch.equal(a, w)
+
+
 def test_two_calls_at_once():
     """Two streams, two problems, in turns; each has its own workspace."""
     work, want = [], []

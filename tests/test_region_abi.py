@@ -119,6 +119,15 @@ def test_binding_names_what_is_wrong():
         sa.slide_dropout_bwd(q, 0.1, 0)
 
 
+def test_binding_names_what_no_plan_can_hold():
+    x = torch.zeros(1, 4, 4, 8)
+    for region in (3, None):
+        with pytest.raises(sa.SlideAttnError, match="q_region"):
+            sa.slide_region_select(x, x, 1, heads=1, q_region=region, k_region=(2, 2))
+    with pytest.raises(sa.SlideAttnError, match="call must be"):
+        sa.slide_region_workspace_bytes("forward", x, x, 1, heads=1, q_region=(2, 2), k_region=(2, 2))
+
+
 def test_strides_of_parts():
     def strides(t, name):
         return region._strides(t.shape, t.stride(), name)
