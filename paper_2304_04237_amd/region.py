@@ -250,12 +250,13 @@ def _attention(q, k, v, index, heads, q_region, k_region, kv_heads, q_size, k_si
         raise SlideAttnError("index must be int32 [B, kv_heads, regions of q, topk]")
     maps = (("k", k), ("v", v))
     plan = _plan(q, maps, heads, q_region, k_region, kv_heads, index.shape[3])
+    # (as the float32 that it becomes: one too small for that would turn into 0, which stands for the default)
+    if scale is not None and not 0.0 < ctypes.c_float(scale).value < float("inf"):
+        raise SlideAttnError("scale must be positive in float32")
     device = _device(q, maps)
     p = plan.problem(q_size, k_size, device)
     p.dropout, p.seed, p.offset, p.offset_device = _random(dropout, seed, offset, device)
     if scale is not None:
-        if not 0.0 < scale < float("inf"):
-            raise SlideAttnError("scale must be positive")
         p.scale = scale
     return plan, p, _like(index, "index", plan.lists, torch.int32, device)
 

@@ -142,3 +142,11 @@ def test_strides_of_parts():
     for bad in (x[:, :, :3], x.permute(0, 2, 1, 3), x[..., ::2]):
         with pytest.raises(sa.SlideAttnError, match="evenly spaced"):
             strides(bad, "x")
+
+
+@pytest.mark.parametrize("scale", [0.0, -1.0, 1e-46, 1e300, float("inf"), float("nan")])
+def test_binding_refuses_scales_that_float32_does_not_hold(scale):
+    """1e-46 is below half of float32's smallest number, 2^-149 = 1.4e-45."""
+    x = torch.zeros(1, 4, 4, 8)
+    with pytest.raises(sa.SlideAttnError, match="scale must be positive"):
+        sa.slide_region_attn_fwd(x, x, x, torch.zeros(1, 1, 4, 1, dtype=torch.int32), heads=1, q_region=(2, 2), k_region=(2, 2), scale=scale)
