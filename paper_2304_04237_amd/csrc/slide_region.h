@@ -94,6 +94,18 @@ struct Args {
     const int* index;                   // [B][kv][qm.regions][T]
 };
 
+// A launch has fewer than 2^32 threads (the runtime refuses more): launch(blocks, first), for as many blocks at a time as that allows.
+template <typename F> inline hipError_t in_launches(long long blocks, int threads, F launch)
+{
+    const long long most = ((1ll << 32) - 1) / threads;
+    for (long long first = 0; first < blocks; first += most) {
+        launch((unsigned)std::min(blocks - first, most), (int)first);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // ---- region selection (slide_region_select.hip)
 size_t select_workspace_bytes(const Args& a);
 hipError_t launch_select(const Args& a, int* index, void* workspace, hipStream_t st);

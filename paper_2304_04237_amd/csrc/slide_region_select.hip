@@ -191,12 +191,12 @@ __device__ __forceinline__ void pick(Get get, int chunks, int T, int* list)
 // 8 s + 2 (lane / 16) and the next; right likewise the region; register r of the result: group 4 r + lane / 16, region lane % 16), then one
 // wave per group.  CHUNKS: regions in a lane's registers; 0: read again from LDS.
 template <int CHUNKS>
-__global__ __launch_bounds__(PICK) void region_pick_kernel(SelectArgs f, int NG, int stride)
+__global__ __launch_bounds__(PICK) void region_pick_kernel(SelectArgs f, int NG, int stride, int first)
 {
     extern __shared__ uint64_t rank[];              // [NG][stride]
     const int G = f.q.m.regions, J = f.k.m.regions, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int per_head = (G + NG - 1) / NG;
-    const int bm = blockIdx.x / per_head, i0 = (blockIdx.x - bm * per_head) * NG, b = bm / f.kv;
+    const int block = blockIdx.x + first, bm = block / per_head, i0 = (block - bm * per_head) * NG, b = bm / f.kv;
     const int col = lane & 15, part = lane >> 4;
     const int gi = min(i0 + min(col, NG - 1), G - 1);
     const double* qp = f.q.sum + ((long long)bm * G + gi) * f.dp + 2 * part;
@@ -290,12 +290,10 @@ static hipError_t run(const Args& a, int* index, unsigned char* ws, hipStream_t 
     f.k.mean = 1;
     f.B = a.B; f.kv = a.kv; f.d = a.d; f.dp = padded(a.d); f.T = a.T;
     f.index = index;
-    hipError_t e;
-    const int pools = f.q.blocks + f.k.blocks, most = (1 << 24) - 1;        // (a launch has fewer than 2^32 threads)
-    for (int first = 0; first < pools; first += most) {
-        region_pool_kernel<T, E><<<std::min(pools - first, most), POOL, 0, st>>>(f, first);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    hipError_t e = in_launches(f.q.blocks + f.k.blocks, POOL, [&](unsigned blocks, int first) {
+        region_pool_kernel<T, E><<<blocks, POOL, 0, st>>>(f, first);
+    });
+    if (e != hipSuccess) return e;
 
     // groups per block: 16 fill a matrix instruction; fewer where their ranks would not let two blocks into a compute unit
     const int J = a.km.regions, stride = (J + 15) / 16 * 16 + 2;
@@ -309,8 +307,7 @@ static hipError_t run(const Args& a, int* index, unsigned char* ws, hipStream_t 
     if (e != hipSuccess) return e;
     const auto kernel = J <= 64 ? region_pick_kernel<1> : J <= 128 ? region_pick_kernel<2> : J <= 256 ? region_pick_kernel<4>
                       : J <= 512 ? region_pick_kernel<8> : J <= 1024 ? region_pick_kernel<16> : region_pick_kernel<0>;
-    kernel<<<blocks, PICK, lds, st>>>(f, NG, stride);
-    return hipGetLastError();
+    return in_launches(blocks, PICK, [&](unsigned n, int first) { kernel<<<n, PICK, lds, st>>>(f, NG, stride, first); });
 }
 
 hipError_t launch_select(const Args& a, int* index, void* workspace, hipStream_t st)
