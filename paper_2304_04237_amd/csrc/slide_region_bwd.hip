@@ -230,13 +230,13 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
 // The lists turned around: a wave per region of keys, or sixteen, each over its part, per N regions where the lists are long, go over
 // all entries of their image and head, first counting, then writing in order.
 template <int N>
-__global__ __launch_bounds__(1024) void region_invert_kernel(BwdArgs f)
+__global__ __launch_bounds__(1024) void region_invert_kernel(BwdArgs f, int first_block)
 {
     const Args& a = f.a;
     __shared__ int less_of[16], mine_of[16][N];
     const int lane = threadIdx.x & 63, J = a.km.regions, units = (J + N - 1) / N;
     const int waves = f.invert_waves, wave = (threadIdx.x >> 6) & (waves - 1), base = (threadIdx.x >> 6) - wave;
-    const long long id = waves == 1 ? (long long)blockIdx.x * 4 + base : blockIdx.x;
+    const long long block = (long long)blockIdx.x + first_block, id = waves == 1 ? block * 4 + base : block;
     const bool live = id < (long long)a.B * a.kv * units;
     const int bm = live ? (int)(id / units) : 0, j = live ? (int)(id - (long long)bm * units) * N : 0;
     const int* list = a.index + (long long)bm * f.entries;
@@ -682,10 +682,12 @@ static hipError_t run_t(BwdArgs& f, unsigned char* ws, hipStream_t st)
     f.invert_waves = f.entries >= 2048 ? 16 : 1;
     const int lists = a.B * a.kv, regions = lists * a.km.regions;
     // Four regions a block where that still fills the chip (8262 regions: 77 us by one, 46 by four; 312: 9.5 and 14).
-    if (f.invert_waves == 1) region_invert_kernel<1><<<(regions + 3) / 4, 256, 0, st>>>(f);
-    else if (regions < 4 * device_cu_count()) region_invert_kernel<1><<<regions, 1024, 0, st>>>(f);
-    else region_invert_kernel<4><<<lists * ((a.km.regions + 3) / 4), 1024, 0, st>>>(f);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (f.invert_waves == 1) region_invert_kernel<1><<<(regions + 3) / 4, 256, 0, st>>>(f, 0);
+    else if (regions < 4 * device_cu_count()) region_invert_kernel<1><<<regions, 1024, 0, st>>>(f, 0);
+    else e = in_launches((long long)lists * ((a.km.regions + 3) / 4), 1024, [&](unsigned blocks, int first) {
+        region_invert_kernel<4><<<blocks, 1024, 0, st>>>(f, first);
+    });
+    if (e != hipSuccess || (e = hipGetLastError()) != hipSuccess) return e;
     return a.d <= 32 ? run_keys<T, 32>(f, st) : a.d <= 64 ? run_keys<T, 64>(f, st) : run_keys<T, 128>(f, st);
 }
 
