@@ -90,7 +90,8 @@ def _like(t, name, shape, dtype, device):
 
 def _random(dropout, seed, offset, device):
     """Rate, seed, number of the call, and where the rest of that number is read from on the device."""
-    if not 0.0 <= dropout < 1.0 - 2.0 ** -17:
+    # (as the float32 that it becomes, which may round up to the limit)
+    if not (dropout >= 0.0 and ctypes.c_float(dropout).value < 1.0 - 2.0 ** -17):
         raise SlideAttnError("dropout must be in [0, 1 - 2^-17)")
     number, holder = (0, offset) if isinstance(offset, torch.Tensor) else (_int(offset, "offset", 0, 2 ** 32 - 1), None)
     if holder is not None:
@@ -151,8 +152,10 @@ class _Plan:
             p.k_size = _like(k_size, "k_size", self.sizes, torch.int32, device)
         return p
 
-    def scratch(self, p, call, workspace, like, index):
-        """Pointer and bytes of the scratch: the caller's, or as much as the call needs (its tensor last)."""
+    def scratch(self, call, workspace, like, index):
+        """Pointer and bytes of the scratch: the caller's, or as much as the call needs (its tensor last).
+
+        The need is asked for once, of the problem without what a call brings along: one that is refused needs nothing."""
         if workspace is not None:
             _on(workspace, "workspace", like.device)
             if not workspace.is_contiguous():
@@ -160,7 +163,7 @@ class _Plan:
             return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
         need = self.need.get((call, index))
         if need is None:
-            need = self.need[(call, index)] = _library().slide_region_workspace_bytes(p, call)
+            need = self.need[(call, index)] = _library().slide_region_workspace_bytes(_Problem.from_buffer_copy(self.image), call)
         if need == 0:
             return None, 0, None
         workspace = like.new_empty((need,), dtype=torch.uint8)
@@ -239,7 +242,7 @@ def slide_region_select(q, k, topk, heads, q_region, k_region, kv_heads=None, q_
         index = q.new_empty(plan.lists, dtype=torch.int32)
     else:
         _like(index, "index", plan.lists, torch.int32, device)
-    ws, size, keep = plan.scratch(p, _SELECT, workspace, q, device.index)
+    ws, size, keep = plan.scratch(_SELECT, workspace, q, device.index)
     _check(lib.slide_region_select(p, q.data_ptr(), k.data_ptr(), index.data_ptr(), ws, size, _stream(device.index)))
     return index
 
@@ -276,7 +279,7 @@ def slide_region_attn_fwd(q, k, v, index, heads, q_region, k_region, kv_heads=No
     else:
         _like(out, "out", q.shape, q.dtype, device)
     lse_at = None if lse is None else _like(lse, "lse", plan.lse, torch.float32, device)
-    ws, size, keep = plan.scratch(p, _FWD, workspace, q, device.index)
+    ws, size, keep = plan.scratch(_FWD, workspace, q, device.index)
     _check(lib.slide_region_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, out.data_ptr(), lse_at, ws, size,
                                      _stream(device.index)))
     return out
@@ -293,7 +296,7 @@ def slide_region_attn_bwd(dout, q, k, v, index, out, lse, heads, q_region, k_reg
     at = [_like(t, name, like.shape, q.dtype, device)
           for t, name, like in ((dout, "dout", q), (out, "out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
     lse_at = _like(lse, "lse", plan.lse, torch.float32, device)
-    ws, size, keep = plan.scratch(p, _BWD, workspace, q, device.index)
+    ws, size, keep = plan.scratch(_BWD, workspace, q, device.index)
     _check(lib.slide_region_attn_bwd(p, at[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), lists, at[1], lse_at, *at[2:], ws, size,
                                      _stream(device.index)))
     return dq, dk, dv
