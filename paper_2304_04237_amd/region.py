@@ -112,6 +112,9 @@ class _Plan:
         if dtype not in _CODES:
             raise SlideAttnError("activations must be float32 or bfloat16, got %s" % dtype)
         p.dtype = _CODES[dtype]
+        k_shape = maps[0][2]
+        if max(*q_shape, *k_shape) >= 2 ** 31:          # (ctypes would keep the low 32 bits)
+            raise SlideAttnError("maps must have sizes below 2^31")
         p.B, p.q_h, p.q_w, channels = q_shape
         p.heads = _int(heads, "heads", 1, 65535)
         p.kv_heads = p.heads if kv_heads is None else _int(kv_heads, "kv_heads", 1, 65535)
@@ -120,7 +123,6 @@ class _Plan:
         p.head_dim = channels // p.heads
         if not 1 <= p.head_dim <= 128:
             raise SlideAttnError("head size must be 1..128")
-        k_shape = maps[0][2]
         for name, kind, shape, stride in maps:
             if len(shape) != 4 or kind != dtype or shape[0] != p.B or shape[3] != p.kv_heads * p.head_dim or shape != k_shape:
                 raise SlideAttnError("%s must be %s [%d, H, W, %d]%s" % (name, str(dtype)[6:], p.B, p.kv_heads * p.head_dim,

@@ -42,3 +42,14 @@ def test_the_largest_dropout_that_float32_holds():
     p = plan_of(q, q).problem(None, None, q.device)
     p.dropout = rate
     assert region._library().slide_region_workspace_bytes(p, region._BWD) > 0
+
+
+@pytest.mark.parametrize("q_shape, k_shape, heads", [
+    ((1, 1, 2 ** 32 + 5, 8), (1, 1, 20, 8), 1), ((1, 2 ** 32 + 5, 1, 8), (1, 1, 20, 8), 1), ((2 ** 32 + 1, 1, 5, 8), (2 ** 32 + 1, 1, 5, 8), 1),
+    ((1, 1, 5, 8), (1, 1, 2 ** 32 + 20, 8), 1), ((1, 1, 5, 8), (1, 2 ** 31, 1, 8), 1), ((1, 1, 5, 2 ** 32 + 32), (1, 1, 5, 2 ** 32 + 32), 1),
+    ((1, 1, 5, 2 ** 33 + 64), (1, 1, 5, 2 ** 33 + 64), 2)])
+def test_sizes_that_an_int_does_not_hold_are_refused(q_shape, k_shape, heads):
+    """The library's sizes are ints: 2^32 + 5 must not arrive there as 5."""
+    q, k = torch.empty(q_shape, device="meta"), torch.empty(k_shape, device="meta")
+    with pytest.raises(sa.SlideAttnError):
+        plan_of(q, k, heads=heads)
