@@ -105,7 +105,7 @@ class _Plan:
     """What follows from the sizes, strides and types of a call: its problem without pointers, the shapes of lists and lse, and
     how much scratch each call needs on each device."""
 
-    def __init__(self, dtype, q_shape, q_stride, maps, heads, q_region, k_region, kv_heads, topk):
+    def __init__(self, dtype, q_shape, q_stride, maps, heads, q_region_h, q_region_w, k_region_h, k_region_w, kv_heads, topk):
         p = _Problem()
         if len(q_shape) != 4:
             raise SlideAttnError("activations must be [B, H, W, C]")
@@ -133,11 +133,8 @@ class _Plan:
         p.q_pixel, p.q_image = _strides(q_shape, q_stride, "q")
         p.k_pixel, p.k_image = _strides(k_shape, maps[0][3], "k")
         p.v_pixel, p.v_image = _strides(k_shape, maps[1][3], "v") if len(maps) > 1 else (0, 0)
-        for name, region in (("q_region", q_region), ("k_region", k_region)):
-            if len(region) != 2:
-                raise SlideAttnError("%s must be (height, width)" % name)
-        p.q_region_h, p.q_region_w = (_int(n, "q_region", 1, 2 ** 31 - 1) for n in q_region)
-        p.k_region_h, p.k_region_w = (_int(n, "k_region", 1, 2 ** 31 - 1) for n in k_region)
+        p.q_region_h, p.q_region_w = (_int(n, "q_region", 1, 2 ** 31 - 1) for n in (q_region_h, q_region_w))
+        p.k_region_h, p.k_region_w = (_int(n, "k_region", 1, 2 ** 31 - 1) for n in (k_region_h, k_region_w))
         p.topk = _int(topk, "topk", 1, 1024)
         groups = -(-p.q_h // p.q_region_h) * -(-p.q_w // p.q_region_w)
         self.image = bytes(p)
@@ -172,16 +169,17 @@ class _Plan:
         return workspace.data_ptr(), need, workspace
 
 
-_plan_of = functools.lru_cache(maxsize=4096)(_Plan)
+# (typed: 2.0 and True are equal to 2 and 1, but are refused)
+_plan_of = functools.lru_cache(maxsize=4096, typed=True)(_Plan)
 
 
 def _plan(q, maps, heads, q_region, k_region, kv_heads, topk):
     """The plan of maps q, k (and v): everything that a kernel relies on is checked once per set of sizes, the devices every time."""
     try:
-        regions = tuple(q_region), tuple(k_region)
-    except TypeError:
+        (qh, qw), (kh, kw) = q_region, k_region
+    except (TypeError, ValueError):
         raise SlideAttnError("q_region and k_region must be (height, width)") from None
-    return _plan_of(q.dtype, q.shape, q.stride(), tuple((n, t.dtype, t.shape, t.stride()) for n, t in maps), heads, *regions, kv_heads, topk)
+    return _plan_of(q.dtype, q.shape, q.stride(), tuple((n, t.dtype, t.shape, t.stride()) for n, t in maps), heads, qh, qw, kh, kw, kv_heads, topk)
 
 
 def _empty(t):

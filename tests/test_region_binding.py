@@ -53,3 +53,17 @@ def test_sizes_that_an_int_does_not_hold_are_refused(q_shape, k_shape, heads):
     q, k = torch.empty(q_shape, device="meta"), torch.empty(k_shape, device="meta")
     with pytest.raises(sa.SlideAttnError):
         plan_of(q, k, heads=heads)
+
+
+@pytest.mark.parametrize("change", [dict(heads=2.0), dict(kv_heads=2.0), dict(q_region=(4.0, 4)), dict(k_region=(4, 4.0)), dict(topk=1.0),
+                                    dict(topk=True), dict(q_region=(True, 4)), dict(heads=True)])
+def test_what_is_no_integer_is_refused_after_an_equal_integer_too(change):
+    """2.0 and True equal 2 and 1: a plan that was made for those must not answer for them."""
+    x = torch.zeros(1, 12, 12, 64)
+    for topk in (1, 2):
+        for heads in (1, 2):
+            for height in (1, 4):
+                plan_of(x, x, topk=topk, heads=heads, q_region=(height, 4))
+                plan_of(x, x, topk=topk, heads=heads, kv_heads=heads, q_region=(height, 4))
+    with pytest.raises(sa.SlideAttnError, match="must be an integer"):
+        plan_of(x, x, **change)
