@@ -335,11 +335,12 @@ int slide_attn_fwd_traffic_probe(const void* q, const void* k, const void* v, vo
  * up to a multiple of 32) over all regions, key heads and images, as many places of key regions likewise, and fewer than 2^30
  * entries in the lists of an image's key head;
  * slide_region_select: at most 16384 regions of keys.
- * SLIDE_ERR_SHAPE otherwise, and for a dropout outside [0, 1) or one that rounds to 1, a negative or NaN scale, and strides that
- * let pixels of one map overlap.  Products are formed from the activations as they are (bf16: exactly), sums and softmax
- * statistics are float32; for bf16 the attention weights and the logits' gradients are rounded to bf16 before the products with
- * v, k, q and dout.  Results are reproducible run to run.  Outputs overlap no input; calls that may overlap in time (on two streams,
- * in two graphs) have workspaces of their own.
+ * SLIDE_ERR_SHAPE otherwise, and for a dropout outside [0, 1) or one that rounds to 1, a negative or NaN scale or one that
+ * float32 does not hold times log2 e (backward: or times 65536 / (65536 - t)), and strides that let pixels of one map overlap.
+ * Products are formed from the activations as they are (bf16: exactly), sums and softmax statistics are float32; for bf16 the
+ * attention weights and the logits' gradients are rounded to bf16 before the products with v, k, q and dout.  Results are
+ * reproducible run to run.  Outputs overlap no input; calls that may overlap in time (on two streams, in two graphs) have
+ * workspaces of their own.
  */
 typedef struct {
     int B, heads, kv_heads, head_dim;

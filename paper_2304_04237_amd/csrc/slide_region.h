@@ -11,6 +11,8 @@
 namespace slide {
 namespace region {
 
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
 // Division of numbers below 2^31 by a number that the host knows: one product.  (n m) >> (31 + s) with m = floor(2^(31 + s) / x) + 1,
 // s = ceil(log2 x), is exact for n < 2^31: m x exceeds 2^(31 + s) by at most x <= 2^s.
 struct Div {

@@ -4,6 +4,7 @@
 #include "slide_region.h"
 
 using slide::region::Args;
+using slide::region::LOG2E;
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
@@ -65,6 +66,8 @@ static int check(const slide_region_problem* p, int call, Args& a)
         if (!strides_fit(p->v_pixel, p->v_image, p->kv_heads * p->head_dim, a.km)) return SLIDE_ERR_SHAPE;
         if (!(p->scale >= 0.0f) || std::isinf(p->scale)) return SLIDE_ERR_SHAPE;
         if (!make_random(p->dropout, p->seed, p->offset, p->offset_device, a.rnd)) return SLIDE_ERR_SHAPE;
+        // what the kernels multiply by: an infinity would make a NaN of every zero
+        if (std::isinf(p->scale * LOG2E) || (call == SLIDE_REGION_BWD && std::isinf(p->scale * a.rnd.scale))) return SLIDE_ERR_SHAPE;
         if (!aligned(p->offset_device, 8)) return SLIDE_ERR_ALIGN;
     }
     if (!aligned(p->q_size, 4) || !aligned(p->k_size, 4)) return SLIDE_ERR_ALIGN;

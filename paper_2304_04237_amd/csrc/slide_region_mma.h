@@ -25,8 +25,6 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 // two floats rounded to bf16 (to nearest, ties to even) in one dword: one instruction
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, bf2)); }
 
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
-
 // row that register r of a product's result is in lane half h
 __device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
