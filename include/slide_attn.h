@@ -331,9 +331,10 @@ int slide_attn_fwd_traffic_probe(const void* q, const void* k, const void* v, vo
  * is at least t (half word 2 w + 1 is the upper half of word w).  offset: the number of the call, plus the low 32 bits of what
  * offset_device (one integer on the device, or NULL) holds when the kernels run: a captured graph draws new masks with it.
  *
- * Limits: head_dim 1..128, topk 1..1024, fewer than 2^29 pixels per map, fewer than 2^24 times 32 rows (rows of a region counted
- * up to a multiple of 32) over all regions, key heads and images, as many places of key regions likewise, and fewer than 2^30
- * entries in the lists of an image's key head;
+ * Limits: head_dim 1..128, topk 1..1024, at most 65535 images, query heads, and key heads over all images, fewer than 2^29 pixels
+ * per map, fewer than 2^24 times 32 rows (rows of a region counted up to a multiple of 32) over all regions, key heads and images,
+ * as many places of key regions likewise, fewer than 2^30 entries in the lists of an image's key head, fewer than 2^31 - 256 places
+ * in one list (those of a region counted up to a multiple of 4), pixels fewer than 2^31 elements apart and images fewer than 2^45;
  * slide_region_select: at most 16384 regions of keys.
  * SLIDE_ERR_SHAPE otherwise, and for a dropout outside [0, 1) or one that rounds to 1, a negative or NaN scale or one that
  * float32 does not hold times log2 e (backward: or times 65536 / (65536 - t)), and strides that let pixels of one map overlap.

@@ -40,7 +40,8 @@ static int check(const slide_region_problem* p, int call, Args& a)
     if (!p) return SLIDE_ERR_NULL;
     if (p->dtype != SLIDE_F32 && p->dtype != SLIDE_BF16) return SLIDE_ERR_DTYPE;
     if (p->B < 1 || p->heads < 1 || p->kv_heads < 1 || p->heads % p->kv_heads != 0) return SLIDE_ERR_SHAPE;
-    if (p->B > 65535 || p->heads > 65535 || (long long)p->B * p->kv_heads > 65535) return SLIDE_ERR_SHAPE;      // grid z
+    // (as the library's other calls; products of these and head sizes stay ints)
+    if (p->B > 65535 || p->heads > 65535 || (long long)p->B * p->kv_heads > 65535) return SLIDE_ERR_SHAPE;
     if (p->head_dim < 1 || p->head_dim > 128 || p->topk < 1 || p->topk > 1024) return SLIDE_ERR_SHAPE;
     a = Args{};
     a.B = p->B; a.heads = p->heads; a.kv = p->kv_heads; a.g = p->heads / p->kv_heads;

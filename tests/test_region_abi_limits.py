@@ -31,3 +31,43 @@ def test_a_scale_that_only_the_backward_cannot_use(lib):  # noqa: F811
 @pytest.mark.parametrize("scale, dropout", [(2.3e38, 0.0), (1e37, 0.9), (1e33, 0.99998), (1e-45, 0.5)])
 def test_scales_that_do_not_are_taken(lib, scale, dropout):  # noqa: F811
     assert taken(lib, BWD, scale=scale, dropout=dropout)
+
+
+def small(**change):
+    """Maps of two pixels, so that batches and heads of any number stay within the other limits."""
+    a = dict(B=1, heads=1, kv_heads=1, head_dim=8, q_h=1, q_w=2, k_h=1, k_w=2, q_region_h=1, q_region_w=2, k_region_h=1, k_region_w=2, topk=1,
+             q_pixel=1 << 20, q_image=1 << 21, k_pixel=1 << 20, k_image=1 << 21, v_pixel=1 << 20, v_image=1 << 21)
+    a.update(change)
+    return a
+
+
+@pytest.mark.parametrize("call", [SELECT, BWD])
+def test_batches_and_heads(lib, call):  # noqa: F811
+    """At most 65535 images, heads, and key heads over all images."""
+    for most, more in [(dict(B=65535), dict(B=65536)), (dict(heads=65535), dict(heads=65536)),
+                       (dict(B=21845, heads=6, kv_heads=3), dict(B=21846, heads=6, kv_heads=3))]:
+        assert taken(lib, call, **small(**most)) and not taken(lib, call, **small(**more))
+
+
+@pytest.mark.parametrize("call", [SELECT, BWD])
+def test_rows_and_places(lib, call):  # noqa: F811
+    """Fewer than 2^24 times 32 rows over all regions, key heads and images, and as many places; fewer than 2^29 pixels a map."""
+    for most, more in [(dict(q_w=(1 << 24) - 1, q_region_w=1), dict(q_w=1 << 24, q_region_w=1)),
+                       (dict(q_w=(1 << 21) - 1, q_region_w=1, heads=8, kv_heads=8), dict(q_w=1 << 21, q_region_w=1, heads=8, kv_heads=8))]:
+        assert taken(lib, call, **small(**most)) and not taken(lib, call, **small(**more))
+    if call == BWD:
+        for most, more in [(dict(k_w=(1 << 24) - 1, k_region_w=1), dict(k_w=1 << 24, k_region_w=1)),
+                           (dict(q_w=1 << 20, q_region_w=1, topk=1023), dict(q_w=1 << 20, q_region_w=1, topk=1024))]:
+            assert taken(lib, call, **small(**most)) and not taken(lib, call, **small(**more))
+    assert not taken(lib, call, **small(q_w=1 << 29)) and not taken(lib, call, **small(k_w=1 << 29))
+
+
+def test_keys_of_a_list_and_strides(lib):  # noqa: F811
+    """Places of a region, counted up to a multiple of 4, times topk: fewer than 2^31 - 256; pixels fewer than 2^31 elements apart, images
+    fewer than 2^45."""
+    wide = dict(k_w=1 << 27, k_region_w=1 << 27)
+    assert taken(lib, BWD, **small(**wide, topk=15)) and not taken(lib, BWD, **small(**wide, topk=16))
+    for name, most in (("pixel", (1 << 31) - 1), ("image", (1 << 45) - 1)):
+        for side in "qkv":
+            assert taken(lib, BWD, **small(**{"%s_%s" % (side, name): most}))
+            assert not taken(lib, BWD, **small(**{"%s_%s" % (side, name): most + 1}))
