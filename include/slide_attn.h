@@ -386,7 +386,8 @@ int slide_region_attn_fwd(const slide_region_problem* p, const void* q, const vo
 /*
  * Gradients of slide_region_attn_fwd (none through the lists): dq [B, q_h, q_w, heads * head_dim], dk and dv
  * [B, k_h, k_w, kv_heads * head_dim], overwritten, zeros where nothing arrives.  out and lse are the forward's results.  With an
- * image stride of 0 the gradients are still those of every image.
+ * image stride of 0 the gradients are still those of every image.  Time for turning the lists around grows with entries times
+ * regions of keys (every four regions read their image's and key head's lists once, or twice if they are in them).
  */
 int slide_region_attn_bwd(const slide_region_problem* p, const void* dout, const void* q, const void* k, const void* v,
                           const int* index, const void* out, const float* lse, void* dq, void* dk, void* dv,

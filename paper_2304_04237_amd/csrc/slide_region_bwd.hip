@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256, 1) void region_dq_kernel(BwdArgs f)
 }
 
 // The lists turned around: a wave per region of keys, or sixteen, each over its part, per N regions where the lists are long, go over
-// all entries of their image and head, first counting, then writing in order.
+// all entries of their image and head, first counting, then writing in order.  So the time grows with entries times regions.
 template <int N>
 __global__ __launch_bounds__(1024) void region_invert_kernel(BwdArgs f, int first_block)
 {
