@@ -90,8 +90,8 @@ def _like(t, name, shape, dtype, device):
 
 def _random(dropout, seed, offset, device):
     """Rate, seed, number of the call, and where the rest of that number is read from on the device."""
-    # (as the float32 that it becomes, which may round up to the limit)
-    if not (dropout >= 0.0 and ctypes.c_float(dropout).value < 1.0 - 2.0 ** -17):
+    # (also as the float32 that it becomes, which may round up to the limit)
+    if not 0.0 <= dropout < 1.0 - 2.0 ** -17 or ctypes.c_float(dropout).value >= 1.0 - 2.0 ** -17:
         raise SlideAttnError("dropout must be in [0, 1 - 2^-17)")
     number, holder = (0, offset) if isinstance(offset, torch.Tensor) else (_int(offset, "offset", 0, 2 ** 32 - 1), None)
     if holder is not None:

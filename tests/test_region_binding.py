@@ -27,7 +27,7 @@ def test_a_refused_call_leaves_the_next_one_its_scratch():
         assert all(x.isfinite().all() for x in sa.slide_region_attn_bwd(q, q, q, q, index, out, lse, **how))
 
 
-@pytest.mark.parametrize("dropout", [1.0 - 2.0 ** -17 - 1e-12, 1.0 - 2.0 ** -17, 1.0, float("nan"), -1e-50])
+@pytest.mark.parametrize("dropout", [1.0 - 2.0 ** -17 - 1e-12, 1.0 - 2.0 ** -17, 1.0, float("nan"), -1e-50, 10 ** 400])
 def test_dropout_is_refused_as_the_float32_that_it_becomes(dropout):
     """1 - 2^-17 - 1e-12 is 1 - 2^-17 in float32, which rounds to 65536 / 65536 (ties to even)."""
     with pytest.raises(sa.SlideAttnError, match="dropout must be"):
